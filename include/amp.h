@@ -209,6 +209,7 @@ enum amp_node_kind {
 };
 #define AMP_ACT_NONE 0
 #define AMP_ACT_RELU 1
+#define AMP_ACT_TANH 2   /* the gated recurrence's candidate (see "Operators on whole arrays") */
 typedef struct amp_node_desc { int32_t rows, cols, n_in, n_out, aux; } amp_node_desc;
 int amp_add_node(amp_ctx *ctx, int kind, const amp_node_desc *desc, int *node_id);
 int amp_connect(amp_ctx *ctx, int src, int src_port, int dst, int dst_port);
@@ -460,6 +461,125 @@ const char *amp_last_error(amp_ctx *ctx);
  * a launch fails. */
 int amp_measure_peaks(void *dev_buf, size_t bytes, void *hip_stream, double *lds_bytes_per_s_per_cu,
                       double *hbm_read_bytes_per_s);
+
+/* ------------------------------------------------ Operators on whole arrays
+ * What a recurrent model trained from a teacher needs beside its matrix
+ * products when it runs over whole token arrays instead of message by
+ * message: the layer norm, the GRU's state update with gates that do not
+ * read the state (Section 2 lists the GRU among the cells; Appendix C has
+ * its update), and a loss layer against a teacher's top logits.  They need
+ * no context.
+ *
+ * Conventions
+ *   - Every array is DEVICE memory, on the device that is current at the
+ *     call; hip_stream is a hipStream_t of that device (NULL = the default
+ *     stream).  A call queues its kernels there and returns without waiting:
+ *     it allocates nothing, copies nothing to or from the host, and can be
+ *     captured into a HIP graph.
+ *   - Arrays are rows of `cols` (hidden, classes) consecutive elements; a
+ *     stride is the distance of two rows, in elements.  Any alignment that
+ *     the element type allows; 16-byte aligned rows are fastest.  An output's
+ *     stride is at least its row length; an input's may be smaller, 0
+ *     repeats one row.
+ *   - An output overlaps no other array of the call, except where a call
+ *     names a pair that may be the same array.  Two arrays that share rows
+ *     of a wider one (one stride, columns of their own) do not overlap.
+ *   - Sums, statistics and states are kept in 32 bits.  A result is rounded
+ *     once, to the nearest.  No atomics on data: a call's results do not
+ *     depend on timing.
+ *   - workspace: scratch memory of at least the bytes that the *_workspace
+ *     call reports, 16-byte aligned, contents arbitrary before and after.
+ *     Calls that may run at the same time (other streams, graphs replayed
+ *     side by side) need workspaces of their own.  NULL where 0 bytes are
+ *     needed.
+ *   - Errors: AMP_EINVAL for a bad argument, AMP_ENOMEM for too small a
+ *     workspace, AMP_EDEVICE when a launch fails; amp_operator_error()
+ *     returns the message of the calling thread's last failed call.
+ *     Nothing has been launched after AMP_EINVAL or AMP_ENOMEM.
+ */
+enum amp_dtype { AMP_F32 = 0, AMP_BF16 = 1, AMP_F16 = 2 };
+const char *amp_operator_error(void);
+
+/* Layer norm over the last axis:
+ *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(var + eps),
+ * mean and var (the mean of the squared deviations) of the row.  weight and
+ * bias (cols floats) may be NULL (ones, zeros); mean and rstd (rows floats,
+ * what the backward pass needs) may be NULL.  eps >= 0.  y may be x (same
+ * address and stride). */
+int amp_layer_norm_forward(int dtype, size_t rows, size_t cols, const void *x, size_t x_stride, const float *weight, const float *bias,
+                           float eps, void *y, size_t y_stride, float *mean, float *rstd, void *hip_stream);
+/* Its gradients: with n = (x - mean) rstd and q = dy weight,
+ *   dx = rstd (q - mean(q) - n mean(q n)),  dweight = sum over rows of dy n,
+ *   dbias = sum over rows of dy
+ * (both set, not added to; either may be NULL).  dx may be dy or x, and NULL
+ * where only the parameters' gradients are wanted.  Without rows dweight and
+ * dbias are zeros. */
+int amp_layer_norm_workspace(int dtype, size_t rows, size_t cols, size_t *bytes);
+int amp_layer_norm_backward(int dtype, size_t rows, size_t cols, const void *dy, size_t dy_stride, const void *x, size_t x_stride,
+                            const float *weight, const float *mean, const float *rstd, void *dx, size_t dx_stride, float *dweight,
+                            float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Sequences packed into the rows of an array: sequence s has the rows
+ * begin[s] .. end[s] - 1.  begin and end are device arrays of n integers of
+ * index_bytes (4 or 8) bytes, ascending and without overlap; end may be
+ * begin + 1 of one array of n + 1 offsets.  Lengths of 0 are allowed, and so
+ * are rows that belong to no sequence (padding, rows behind the last one):
+ * their outputs are left as they were.  Bounds outside the rows are taken for
+ * the nearest row, and outputs of sequences that overlap or descend are
+ * unspecified.  begin = end = NULL: one sequence (n = 1) of all rows. */
+typedef struct amp_sequences {
+  size_t n;
+  const void *begin, *end;
+  int32_t index_bytes;
+} amp_sequences;
+
+/* Gated linear recurrence: per feature
+ *   z_t = sigmoid(gate_t), v_t = act(cand_t), h_t = (1 - z_t) h_{t-1} + z_t v_t
+ * along every sequence (fewer than 2^30 rows, hidden below 2^22), h before its first row = h0[s] (n x hidden floats;
+ * NULL = zeros): the GRU's update of its state, the gates formed from the
+ * inputs alone.  activation: AMP_ACT_NONE or AMP_ACT_TANH.  h (may be NULL)
+ * gets every row's state in the inputs' type; last (n x hidden floats, may be
+ * NULL) the state behind every sequence's last row, h0 for an empty one.  carry (may be NULL): the states that the backward pass
+ * starts from, amp_gated_scan_carry rows x hidden floats. */
+int amp_gated_scan_carry(int dtype, size_t rows, size_t hidden, size_t *carry_rows);
+int amp_gated_scan_workspace(int dtype, size_t rows, size_t hidden, size_t *bytes);   /* of either direction */
+int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden, const void *gate, size_t gate_stride, const void *cand,
+                           size_t cand_stride, const amp_sequences *sequences, const float *h0, void *h, size_t h_stride, float *last,
+                           float *carry, void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Its gradients.  dh: gradient of every row's state, dlast (n x hidden
+ * floats, may be NULL): of the last states; carry: as the forward pass left
+ * it for the same inputs.  With G_t = dh_t + (1 - z_{t+1}) G_{t+1}, G_{last} =
+ * dh_{last} + dlast:  dgate = G z (1 - z) (v - h_{t-1}),
+ * dcand = G z act'(cand), dh0[s] (may be NULL) = (1 - z) G at
+ * the first row, dlast (or 0) for an empty sequence. */
+int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidden, const void *dh, size_t dh_stride, const float *dlast,
+                            const void *gate, size_t gate_stride, const void *cand, size_t cand_stride, const amp_sequences *sequences,
+                            const float *h0, const float *carry, void *dgate, size_t dgate_stride, void *dcand, size_t dcand_stride,
+                            float *dh0, void *workspace, size_t workspace_bytes, void *hip_stream);
+/* One row of each of `rows` sequences: state = (1 - z) state + z v in place
+ * (32 bits, state_stride floats apart), and its rounded copy in h (may be
+ * NULL). */
+int amp_gated_scan_step(int dtype, int activation, size_t rows, size_t hidden, const void *gate, size_t gate_stride, const void *cand,
+                        size_t cand_stride, float *state, size_t state_stride, void *h, size_t h_stride, void *hip_stream);
+
+/* Distillation from a teacher's top logits, the loss and the gradient that
+ * starts backpropagation in one call (as the loss layers of Section 4 do).
+ * A row has `top` (1 .. 1024) teacher entries, a logit teacher[k] (of type
+ * teacher_dtype) and the class index[k] it belongs to (index_bytes 4 or 8); an
+ * entry is left out where its class is outside 0 .. classes - 1 or its logit
+ * is -infinity.  With p the softmax of the entries' teacher / temperature and
+ * q that of the student's logits / temperature over all classes:
+ *   loss = weight temperature^2 sum_k p_k (log p_k - log q[index_k])
+ *   dlogits_j = weight temperature (q_j - sum of the p_k with index_k = j)
+ * weight: a float per row (NULL = 1); a row of weight 0 is not read, it and a
+ * row whose entries are all left out have a loss and a gradient of 0.  loss:
+ * a float per row (may be NULL); dlogits (NULL: the loss alone) may be logits
+ * (same address and stride). */
+int amp_distill_workspace(int dtype, size_t rows, size_t classes, size_t *bytes);
+int amp_distill_loss(int dtype, size_t rows, size_t classes, const void *logits, size_t logits_stride, size_t top, int teacher_dtype,
+                     const void *teacher, size_t teacher_stride, const void *index, int index_bytes, size_t index_stride,
+                     float temperature, const float *weight, float *loss, void *dlogits, size_t dlogits_stride, void *workspace,
+                     size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -48,7 +48,8 @@ class NodeDesc(ct.Structure):
 NODE_KINDS = ("controller", "lookup", "linear", "rnn_tanh", "gru", "leaf_lstm", "branch_lstm", "ggnn_edge_linear",
               "sum_readout", "softmax_xent", "squared_err", "cond", "phi", "isu", "concat", "split", "bcast", "group",
               "ungroup", "flatmap", "sum", "sink")
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_TANH = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
 
 
 class OptParams(ct.Structure):
@@ -65,7 +66,12 @@ class EvalResult(ct.Structure):
                 ("n_predictions", ct.c_uint64), ("seconds", ct.c_double)]
 
 
+class Sequences(ct.Structure):
+    _fields_ = [("n", ct.c_size_t), ("begin", ct.c_void_p), ("end", ct.c_void_p), ("index_bytes", ct.c_int32)]
+
+
 _ctxp = ct.c_void_p
+_i, _n, _p, _f = ct.c_int, ct.c_size_t, ct.c_void_p, ct.c_float   # operators' arguments: int, size or stride, device pointer, float
 SIGNATURES = {
     "amp_create": (ct.c_int, [ct.POINTER(_ctxp), ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "amp_create_static": (ct.c_int, [ct.POINTER(_ctxp), ct.c_void_p]),
@@ -116,6 +122,18 @@ SIGNATURES = {
     "amp_last_error": (ct.c_char_p, [_ctxp]),
     "amp_measure_peaks": (ct.c_int, [ct.c_void_p, ct.c_size_t, ct.c_void_p, ct.POINTER(ct.c_double),
                                      ct.POINTER(ct.c_double)]),
+    "amp_operator_error": (ct.c_char_p, []),
+    "amp_layer_norm_forward": (_i, [_i, _n, _n, _p, _n, _p, _p, _f, _p, _n, _p, _p, _p]),
+    "amp_layer_norm_workspace": (_i, [_i, _n, _n, ct.POINTER(_n)]),
+    "amp_layer_norm_backward": (_i, [_i, _n, _n, _p, _n, _p, _n, _p, _p, _p, _p, _n, _p, _p, _p, _n, _p]),
+    "amp_gated_scan_carry": (_i, [_i, _n, _n, ct.POINTER(_n)]),
+    "amp_gated_scan_workspace": (_i, [_i, _n, _n, ct.POINTER(_n)]),
+    "amp_gated_scan_forward": (_i, [_i, _i, _n, _n, _p, _n, _p, _n, ct.POINTER(Sequences), _p, _p, _n, _p, _p, _p, _n, _p]),
+    "amp_gated_scan_backward": (_i, [_i, _i, _n, _n, _p, _n, _p, _p, _n, _p, _n, ct.POINTER(Sequences), _p, _p, _p, _n, _p, _n, _p, _p,
+                                     _n, _p]),
+    "amp_gated_scan_step": (_i, [_i, _i, _n, _n, _p, _n, _p, _n, _p, _n, _p, _n, _p]),
+    "amp_distill_workspace": (_i, [_i, _n, _n, ct.POINTER(_n)]),
+    "amp_distill_loss": (_i, [_i, _n, _n, _p, _n, _n, _i, _p, _n, _p, _i, _n, _f, _p, _p, _p, _n, _p, _n, _p]),
 }
 
 _libs = {}
