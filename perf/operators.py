@@ -246,8 +246,14 @@ def _run_own(s):
         h, last, carry = ops.gated_scan(s["gate"], s["cand"], s["offsets"], h0=s["h0"], activation=s["act"], last=True, carry=train)
         if not train:
             return h, last
-        return (h, last) + ops.gated_scan_backward(s["dh"], s["gate"], s["cand"], carry, s["offsets"], h0=s["h0"], dlast=s["dlast"],
-                                                   activation=s["act"])
+        grads = ops.gated_scan_backward(s["dh"], s["gate"], s["cand"], carry, s["offsets"], h0=s["h0"], dlast=s["dlast"],
+                                        activation=s["act"])
+        if s["dh"].dtype == torch.float32:
+            # the plain form adds dlast to dh in place where dh is in 32 bits: a pass leaves the same behind, so that further
+            # passes over one state have the same inputs in both
+            begin, end = s["offsets"][:-1], s["offsets"][1:]
+            s["dh"].index_add_(0, (end - 1).clamp_(min=0), s["dlast"] * (end > begin)[:, None])
+        return (h, last) + grads
     loss, grad = ops.distill_loss(s["logits"], s["teacher"], s["index"], s["temperature"], s["weight"], grad=s["mode"] == "train")
     return loss if grad is None else (loss, grad)
 
