@@ -535,7 +535,7 @@ typedef struct amp_sequences {
 
 /* Gated linear recurrence: per feature
  *   z_t = sigmoid(gate_t), v_t = act(cand_t), h_t = (1 - z_t) h_{t-1} + z_t v_t
- * along every sequence (fewer than 2^30 rows, hidden below 2^22), h before its first row = h0[s] (n x hidden floats;
+ * along every sequence (fewer than 2^30 rows, hidden and strides below 2^22), h before its first row = h0[s] (n x hidden floats;
  * NULL = zeros): the GRU's update of its state, the gates formed from the
  * inputs alone.  activation: AMP_ACT_NONE or AMP_ACT_TANH.  h (may be NULL)
  * gets every row's state in the inputs' type; last (n x hidden floats, may be

@@ -108,6 +108,11 @@ int check_scan_size(const char* what, int dtype, size_t rows, size_t hidden) {
   return AMP_OK;
 }
 
+// The scan's kernels reach a tile's rows by 32-bit offsets.
+int check_scan_stride(const char* what, const char* name, size_t stride) {
+  return stride < (size_t)1 << 22 ? AMP_OK : fail(AMP_EINVAL, "%s: %s has a row stride of 2^22 or more", what, name);
+}
+
 int check_scan(const char* what, int dtype, int activation, size_t rows, size_t hidden, const amp_sequences* q) {
   CHECK(check_scan_size(what, dtype, rows, hidden));
   if (activation != AMP_ACT_NONE && activation != AMP_ACT_TANH)
@@ -226,6 +231,9 @@ int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden
                     {"h0", h0, n, hidden, hidden, 4},             {"begin", q->begin, 1, n, n, q->begin ? ib : 1},
                     {"end", q->end, 1, n, n, q->end ? ib : 1}};
   CHECK(check_arrays(what, s, 4));
+  CHECK(check_scan_stride(what, "gate", gate_stride));
+  CHECK(check_scan_stride(what, "cand", cand_stride));
+  CHECK(check_scan_stride(what, "h", h_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 4, nullptr, 0));
   ScanArgs a = {};
@@ -259,6 +267,11 @@ int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidde
                     {"h0", h0, n, hidden, hidden, 4},                {"carry", carry, nc, hidden, hidden, 4},
                     {"begin", q->begin, 1, n, n, q->begin ? ib : 1}, {"end", q->end, 1, n, n, q->end ? ib : 1}};
   CHECK(check_arrays(what, s, 4));
+  CHECK(check_scan_stride(what, "dh", dh_stride));
+  CHECK(check_scan_stride(what, "gate", gate_stride));
+  CHECK(check_scan_stride(what, "cand", cand_stride));
+  CHECK(check_scan_stride(what, "dgate", dgate_stride));
+  CHECK(check_scan_stride(what, "dcand", dcand_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 4, nullptr, 0));
   ScanArgs a = {};

@@ -11,34 +11,42 @@ typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef f16 v2h __attribute__((ext_vector_type(2)));
 
-// A group of 16 bytes, the widest access of a lane.  Rows start at any element (odd lengths, views): the hardware takes 16-byte
-// accesses at any address, at a second cache line's cost where one is crossed, so there is no path for unaligned rows.
-template <class T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
-  v4u u;
+// A group of N elements, 16 bytes (the widest access of a lane) or 8.  Rows start at any element (odd lengths, views): the hardware
+// takes such accesses at any address, at a second cache line's cost where one is crossed, so there is no path for unaligned rows.
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+template <int WORDS>
+struct Words;
+template <>
+struct Words<4> {
+  typedef v4u type;
 };
-typedef v4u v4u_any __attribute__((aligned(2)));
-typedef v4u v4u_word __attribute__((aligned(4)));
+template <>
+struct Words<2> {
+  typedef v2u type;
+};
+template <class T, int N_ = 16 / sizeof(T)>
+struct Vec {
+  static constexpr int N = N_;
+  typedef typename Words<N * sizeof(T) / 4>::type U;
+  typedef U Any __attribute__((aligned(sizeof(T))));
+  U u;
+};
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(bf16 v) { return (float)v; }
 __device__ __forceinline__ float widen(f16 v) { return (float)v; }
 
 // The group at p, elements n and later replaced by zeros and not read (n >= N: all of it).
-template <class T>
-__device__ __forceinline__ Vec<T> load_vec(const T* p, long n) {
-  Vec<T> v;
-  if (n >= Vec<T>::N) {
-    if (sizeof(T) == 2)
-      v.u = *(const v4u_any*)p;
-    else
-      v.u = *(const v4u_word*)p;
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> load_group(const T* p, long n) {
+  Vec<T, N> v;
+  if (n >= N) {
+    v.u = *(const typename Vec<T, N>::Any*)p;
     return v;
   }
-  v.u = (v4u){0, 0, 0, 0};
+  v.u = (typename Vec<T, N>::U)0u;
 #pragma unroll
-  for (int k = 0; k < Vec<T>::N; ++k)
+  for (int k = 0; k < N; ++k)
     if (k < n) {
       if (sizeof(T) == 2)
         v.u[k / 2] |= (unsigned)((const unsigned short*)p)[k] << (16 * (k & 1));
@@ -47,18 +55,17 @@ __device__ __forceinline__ Vec<T> load_vec(const T* p, long n) {
     }
   return v;
 }
-
 template <class T>
-__device__ __forceinline__ void store_vec(T* p, Vec<T> v, long n) {
-  if (n >= Vec<T>::N) {
-    if (sizeof(T) == 2)
-      *(v4u_any*)p = v.u;
-    else
-      *(v4u_word*)p = v.u;
+__device__ __forceinline__ Vec<T> load_vec(const T* p, long n) { return load_group<16 / sizeof(T)>(p, n); }
+
+template <class T, int N>
+__device__ __forceinline__ void store_vec(T* p, Vec<T, N> v, long n) {
+  if (n >= N) {
+    *(typename Vec<T, N>::Any*)p = v.u;
     return;
   }
 #pragma unroll
-  for (int k = 0; k < Vec<T>::N; ++k)
+  for (int k = 0; k < N; ++k)
     if (k < n) {
       if (sizeof(T) == 2)
         ((unsigned short*)p)[k] = (unsigned short)(v.u[k / 2] >> (16 * (k & 1)));
@@ -67,40 +74,29 @@ __device__ __forceinline__ void store_vec(T* p, Vec<T> v, long n) {
     }
 }
 
-template <class T>
-__device__ __forceinline__ float get(const Vec<T>& v, int k);
-template <>
-__device__ __forceinline__ float get<float>(const Vec<float>& v, int k) { return __uint_as_float(v.u[k]); }
-template <>
-__device__ __forceinline__ float get<bf16>(const Vec<bf16>& v, int k) {
+template <int N>
+__device__ __forceinline__ float get(const Vec<float, N>& v, int k) { return __uint_as_float(v.u[k]); }
+template <int N>
+__device__ __forceinline__ float get(const Vec<bf16, N>& v, int k) {
   const unsigned w = v.u[k / 2];
   return __uint_as_float((k & 1) ? w & 0xffff0000u : w << 16);
 }
-template <>
-__device__ __forceinline__ float get<f16>(const Vec<f16>& v, int k) { return (float)__builtin_bit_cast(v2h, (unsigned)v.u[k / 2])[k & 1]; }
+template <int N>
+__device__ __forceinline__ float get(const Vec<f16, N>& v, int k) { return (float)__builtin_bit_cast(v2h, (unsigned)v.u[k / 2])[k & 1]; }
 
 // N floats rounded to the nearest of T, the one rounding of a result.
-template <class T>
-__device__ __forceinline__ Vec<T> pack(const float (&f)[Vec<T>::N]);
-template <>
-__device__ __forceinline__ Vec<float> pack<float>(const float (&f)[4]) {
-  Vec<float> v;
+__device__ __forceinline__ unsigned pack2(float a, float b, bf16) { return __builtin_bit_cast(unsigned, __builtin_convertvector((v2f){a, b}, v2bf)); }
+__device__ __forceinline__ unsigned pack2(float a, float b, f16) { return __builtin_bit_cast(unsigned, __builtin_convertvector((v2f){a, b}, v2h)); }
+template <class T, int N>
+__device__ __forceinline__ Vec<T, N> pack(const float (&f)[N]) {
+  Vec<T, N> v;
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v.u[k] = __float_as_uint(f[k]);
-  return v;
-}
-template <>
-__device__ __forceinline__ Vec<bf16> pack<bf16>(const float (&f)[8]) {
-  Vec<bf16> v;
+    for (int k = 0; k < N; ++k) v.u[k] = __float_as_uint(f[k]);
+  } else {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v.u[k] = __builtin_bit_cast(unsigned, __builtin_convertvector((v2f){f[2 * k], f[2 * k + 1]}, v2bf));
-  return v;
-}
-template <>
-__device__ __forceinline__ Vec<f16> pack<f16>(const float (&f)[8]) {
-  Vec<f16> v;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v.u[k] = __builtin_bit_cast(unsigned, __builtin_convertvector((v2f){f[2 * k], f[2 * k + 1]}, v2h));
+    for (int k = 0; k < N / 2; ++k) v.u[k] = pack2(f[2 * k], f[2 * k + 1], T());
+  }
   return v;
 }
 
@@ -153,9 +149,9 @@ inline hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, unsigned l
   return hipLaunchKernel((const void*)kernel, grid, block, args, lds, stream);
 }
 
-#define OPS_BY_TYPE(dtype, call)                 \
+#define OPS_BY_TYPE(dtype, ...)                  \
   switch (dtype) {                               \
-    case 0: { typedef float T; call; } break;    \
-    case 1: { typedef bf16 T; call; } break;     \
-    default: { typedef f16 T; call; } break;     \
+    case 0: { typedef float T; __VA_ARGS__; } break;    \
+    case 1: { typedef bf16 T; __VA_ARGS__; } break;     \
+    default: { typedef f16 T; __VA_ARGS__; } break;     \
   }

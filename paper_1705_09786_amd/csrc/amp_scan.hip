@@ -4,16 +4,27 @@
 // h -> P h + Q per feature, and maps compose, so that tiles need not wait for each other's rows.  A row that begins a sequence
 // takes in h0 and is a cut: its map ignores what comes in (P = -0, which no product of the keeps 1 - z >= 0 gives), so that what
 // stands in another sequence, infinities and NaN included, never reaches it.
+//
+// One pass over the data: a workgroup reads a tile once, publishes its map as one 64-bit word per feature, finds the state that
+// comes in from the words of the tiles in front, and writes its rows.  A word is {P, Q}; once the state behind the tile is known it
+// is replaced by the map that gives it, {cut, state}, so a reader goes back to the nearest cut and applies the maps from there on
+// in the rows' order.  Each state is one fma of the state in front of it whichever word a reader met: results do not depend on timing.
 #include "amp_ops.hip.h"
 #include "amp_common.hip.h"
 
 namespace {
 
-constexpr int TPB = 256, TILE = 128, CH = 64;
+constexpr int TPB = 256, TILE = 128, CARRY = TILE;   // the forward pass leaves the state in front of every tile for the backward pass
 
-template <class T>
+// A tile of TILE rows and CH features in a workgroup: V features of a row to a lane, LS rows one behind the other.  V is four in every
+// type: 8-byte groups of 16-bit elements have half the maps to join inside a tile that 16-byte groups have (65,536 x 2,048 bf16,
+// forward: 221 us with groups of 16 bytes, 187 with these), and 64 features of 16 bits are whole cache lines still.
+template <class T, bool NARROW_>
 struct Lay {
-  static constexpr int V = Vec<T>::N, LANES = CH / V, TG = TPB / LANES, LS = TILE / TG;
+  typedef T E;
+  static constexpr bool NARROW = NARROW_;   // rows shorter than V
+  static constexpr int V = 4, CH = 64, LANES = CH / V, TG = TPB / LANES, LS = TILE / TG, PARTS = TPB / CH;
+  static_assert(LS % 4 == 0 && TG % PARTS == 0 && CH == 64, "flags by words, a slot to a lane of one wave");
 };
 
 constexpr unsigned CUT = 0x80000000u;
@@ -29,9 +40,11 @@ __device__ __forceinline__ void compose(float& p, float& q, float p2, float q2) 
 
 // z = 1 / (1 + e^-g) and keep = 1 - z, both exact to the last bits however near to 0 they are; 0 and 1 at infinite g.
 __device__ __forceinline__ void gate_of(float g, float& z, float& keep) {
-  const float s = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + s), small = s * r;
-  z = g >= 0.f ? r : small;
-  keep = g >= 0.f ? small : r;
+  const float s = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + s);
+  // the larger one as 1 - s r: the estimate's error counts s times, not once in every row that a state is kept for
+  const float small = s * r, large = fmaf(-s, r, 1.f);
+  z = g >= 0.f ? large : small;
+  keep = g >= 0.f ? small : large;
 }
 
 __device__ __forceinline__ long bound_at(const void* p, int bytes, size_t s, long lo, long hi) {
@@ -40,15 +53,14 @@ __device__ __forceinline__ long bound_at(const void* p, int bytes, size_t s, lon
 }
 
 struct TileRows {
-  int seq[TILE];              // the sequence of a row, where it has one
-  unsigned char flag[TILE];   // FIRST, LAST, VALID
+  int seq[TILE];                         // the sequence of a row, where it has one
+  alignas(16) unsigned char flag[TILE];  // FIRST, LAST, VALID
   int part[TPB / 64];
 };
 
 // Fills in the tile's rows.  Returns the sequences [s0, s1) that begin in the tile; those behind the last row belong to the last
 // tile.  Sorted bounds give every row its sequence; unsorted ones give it some sequence, and no access leaves its array.
-template <class A>
-__device__ __forceinline__ void tile_rows(const A& a, long t0, TileRows& t, size_t& s0, size_t& s1) {
+__device__ __forceinline__ void tile_rows(const ScanArgs& a, long t0, TileRows& t, size_t& s0, size_t& s1) {
   const long rows = (long)a.rows, t1 = t0 + TILE;
   const int i = threadIdx.x;
   if (!a.begin) {
@@ -110,281 +122,570 @@ __device__ __forceinline__ void tile_rows(const A& a, long t0, TileRows& t, size
   __syncthreads();
 }
 
-// A thread's rows and features.
-template <class T>
+// A thread's rows and features.  Features are independent, so a row's last lanes, where they would pass its end, take its last V
+// features over again: they read, compute and write the same bits as the lanes that own them, and no access is cut short.  A
+// feature's place in its workgroup (its slot) is its own all the same.  (Rows shorter than V: NARROW, element by element.)
+template <class L>
 struct Place {
-  int lane, grp;
-  long row;       // its first row in the array, row - t0 = grp * LS
-  size_t ch;      // its first feature
-  long n;         // features from there on
-  __device__ Place(long t0, size_t c0, size_t hidden) {
-    lane = threadIdx.x % Lay<T>::LANES;
-    grp = threadIdx.x / Lay<T>::LANES;
-    row = t0 + grp * Lay<T>::LS;
-    ch = c0 + lane * Lay<T>::V;
-    n = (long)hidden - (long)ch;
+  int grp, slot;
+  size_t ch;   // its first feature
+  int n;       // NARROW: features from there on
+  __device__ Place(size_t c0, size_t hidden) {
+    slot = threadIdx.x % L::LANES * L::V;
+    grp = threadIdx.x / L::LANES;
+    ch = c0 + slot;
+    n = L::V;
+    if (L::NARROW) {
+      n = ch < hidden ? (int)(hidden - ch) : 0;
+      if (!n) ch = 0;
+    } else if (ch + L::V > hidden) {
+      ch = hidden - L::V;
+    }
   }
 };
 
-template <class T>
-__device__ __forceinline__ void load_rows(const void* p, size_t stride, const Place<T>& at, long rows, Vec<T> (&v)[Lay<T>::LS]) {
+// The feature of a slot.
+template <class L>
+__device__ __forceinline__ size_t feature_of(int slot, size_t c0, size_t hidden) {
+  const size_t ch = c0 + slot / L::V * L::V;
+  return (!L::NARROW && ch + L::V > hidden ? hidden - L::V : ch) + slot % L::V;
+}
+
+// The groups of a tile's array: the tile's first row for all (in scalar registers), 32-bit offsets for the lanes.
+template <class L, class E>
+struct TileArray {
+  E* base;
+  unsigned off, step;
+  __device__ TileArray(E* p, size_t stride, size_t tile, const Place<L>& at) {
+    base = p + tile * TILE * stride;
+    off = (unsigned)(at.grp * L::LS) * (unsigned)stride + (unsigned)at.ch;
+    step = (unsigned)stride;
+  }
+  __device__ E* row(int i) const { return (E*)((char*)base + (off + i * step) * (unsigned)sizeof(E)); }
+};
+
+template <class L>
+__device__ __forceinline__ void load_rows(const void* p, size_t stride, const Place<L>& at, size_t tile, int rows, Vec<typename L::E, L::V> (&v)[L::LS]) {
+  const TileArray<L, const typename L::E> a((const typename L::E*)p, stride, tile, at);
 #pragma unroll
-  for (int i = 0; i < Lay<T>::LS; ++i) {
-    const long r = at.row + i;
-    v[i] = load_vec(row_of((const T*)p, r < rows ? r : 0, stride) + (at.n > 0 ? at.ch : 0), r < rows ? at.n : 0);
+  for (int i = 0; i < L::LS; ++i) {
+    v[i].u = (typename Vec<typename L::E, L::V>::U)0u;
+    if (at.grp * L::LS + i < rows) v[i] = load_group<L::V>(a.row(i), L::NARROW ? at.n : L::V);
   }
 }
 
-__device__ __forceinline__ float state_at(const float* p, int seq, size_t hidden, size_t ch, long n) {
-  return p && n > 0 ? p[(size_t)seq * hidden + ch] : 0.f;
+// A thread's features of a state, in 32 bits.
+template <class L>
+struct State {
+  Vec<float> v[L::V / 4];
+  __device__ float at(int k) const { return get(v[k / 4], k % 4); }
+};
+template <class L>
+__device__ __forceinline__ State<L> load_state(const float* p, size_t row, const ScanArgs& a, const Place<L>& at) {
+  State<L> s;
+#pragma unroll
+  for (int j = 0; j < L::V / 4; ++j) s.v[j] = load_vec(p + row * a.hidden + at.ch + 4 * j, L::NARROW ? at.n - 4 * j : 4);
+  return s;
+}
+template <class L>
+__device__ __forceinline__ void store_state(float* p, size_t row, const ScanArgs& a, const Place<L>& at, const float (&h)[L::V]) {
+#pragma unroll
+  for (int j = 0; j < L::V / 4; ++j) {
+    const float o[4] = {h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]};
+    store_vec(p + row * a.hidden + at.ch + 4 * j, pack<float>(o), L::NARROW ? at.n - 4 * j : 4);
+  }
 }
 
-// The maps of a thread's rows, forward: keep h + z v, cuts taking in h0.
-template <class T, bool TANH>
-__device__ __forceinline__ void row_maps(const ScanArgs& a, const TileRows& t, const Place<T>& at, const Vec<T> (&g)[Lay<T>::LS],
-                                         const Vec<T> (&c)[Lay<T>::LS], float (&p)[Lay<T>::LS][Lay<T>::V],
-                                         float (&q)[Lay<T>::LS][Lay<T>::V]) {
+// A thread's flags, one byte a row; whether all rows of its wave are inner rows of a sequence.
+template <class L>
+struct Flags {
+  unsigned w[L::LS / 4];
+  bool plain;
+  __device__ Flags(const TileRows& t, const Place<L>& at) {
+    plain = true;
 #pragma unroll
-  for (int i = 0; i < Lay<T>::LS; ++i) {
-    const int r = at.grp * Lay<T>::LS + i, f = t.flag[r];
+    for (int i = 0; i < L::LS / 4; ++i) {
+      w[i] = ((const unsigned*)t.flag)[at.grp * (L::LS / 4) + i];
+      plain = plain && w[i] == 0x01010101u * (unsigned)VALID;
+    }
+    plain = __all(plain);
+  }
+  __device__ int of(int i) const { return w[i / 4] >> (i % 4 * 8) & 0xff; }
+};
+
+// The states of a thread's rows with `flag` join what x holds: x + s, or x + keep s.  Four rows' loads are on their way together.
+template <bool KEEP, class L>
+__device__ __forceinline__ void take_in(const float* states, int flag, const ScanArgs& a, const TileRows& t, const Place<L>& at, const Flags<L>& f,
+                                        const float (&keep)[L::LS][L::V], float (&x)[L::LS][L::V]) {
 #pragma unroll
-    for (int k = 0; k < Lay<T>::V; ++k) {
-      float z, v = get(c[i], k);
-      gate_of(get(g[i], k), z, p[i][k]);
-      if (TANH) v = tanh_(v);
-      q[i][k] = z * v;
-      if (f != VALID) {
-        if (f & FIRST) q[i][k] = fmaf(p[i][k], state_at(a.h0, t.seq[r], a.hidden, at.ch + k, at.n - k), q[i][k]);
-        if (!(f & VALID)) q[i][k] = 0.f;
-        if ((f & FIRST) || !(f & VALID)) p[i][k] = __uint_as_float(CUT);
-      }
+  for (int i0 = 0; i0 < L::LS; i0 += 4) {
+    State<L> s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (f.of(i0 + i) & flag) s[i] = load_state<L>(states, t.seq[at.grp * L::LS + i0 + i], a, at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (f.of(i0 + i) & flag)
+#pragma unroll
+        for (int k = 0; k < L::V; ++k) x[i0 + i][k] = KEEP ? fmaf(keep[i0 + i][k], s[i].at(k), x[i0 + i][k]) : x[i0 + i][k] + s[i].at(k);
+  }
+}
+
+// The map of a thread's rows, from the first on.  A cut stays one by itself: -0 times a keep is -0.
+template <bool PLAIN, class L>
+__device__ __forceinline__ void map_forward(const Flags<L>& f, const float (&keep)[L::LS][L::V], const float (&zv)[L::LS][L::V], float (&p)[L::V],
+                                            float (&q)[L::V]) {
+#pragma unroll
+  for (int k = 0; k < L::V; ++k) p[k] = 1.f, q[k] = 0.f;
+#pragma unroll
+  for (int i = 0; i < L::LS; ++i) {
+    const bool cut = !PLAIN && (f.of(i) & (FIRST | VALID)) != VALID, none = !PLAIN && !(f.of(i) & VALID);
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) {
+      const float pk = p[k] * keep[i][k], qk = fmaf(keep[i][k], q[k], zv[i][k]);
+      p[k] = cut ? __uint_as_float(CUT) : pk;
+      q[k] = cut ? (none ? 0.f : zv[i][k]) : qk;
+    }
+  }
+}
+
+// The map of X over a thread's rows, from the last on.
+template <bool PLAIN, class L>
+__device__ __forceinline__ void map_back(const Flags<L>& f, const float (&keep)[L::LS][L::V], const float (&d)[L::LS][L::V], float (&p)[L::V],
+                                         float (&q)[L::V]) {
+#pragma unroll
+  for (int k = 0; k < L::V; ++k) p[k] = 1.f, q[k] = 0.f;
+#pragma unroll
+  for (int i = L::LS - 1; i >= 0; --i) {
+    const bool cut = !PLAIN && (f.of(i) & (FIRST | VALID)) != VALID;
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) {
+      p[k] = cut ? __uint_as_float(CUT) : p[k] * keep[i][k];
+      q[k] = cut ? 0.f : keep[i][k] * (q[k] + d[i][k]);
     }
   }
 }
 
 // Per feature, the map of every thread's rows in front of its own (BACK: behind) inside the tile, and the tile's: through LDS, a
-// quarter of the row groups to a wave, a feature to a lane.
-template <int TG>
-struct Maps {
-  float p[TG][CH], q[TG][CH], tp[4][CH], tq[4][CH];
+// part of the row groups and a feature to a lane.
+template <class L>
+struct __attribute__((aligned(16))) Maps {
+  float p[L::TG][L::CH], q[L::TG][L::CH], tp[L::PARTS][L::CH], tq[L::PARTS][L::CH];
 };
-template <class T, bool BACK>
-__device__ __forceinline__ void scan_groups(Maps<Lay<T>::TG>& m, const Place<T>& at, const float (&p)[Lay<T>::V], const float (&q)[Lay<T>::V]) {
-  constexpr int V = Lay<T>::V, TG = Lay<T>::TG;
+template <class L, bool BACK>
+__device__ __forceinline__ void scan_groups(Maps<L>& m, const Place<L>& at, const float (&p)[L::V], const float (&q)[L::V]) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    m.p[at.grp][at.lane * V + k] = p[k];
-    m.q[at.grp][at.lane * V + k] = q[k];
+  for (int k = 0; k < L::V; ++k) {
+    m.p[at.grp][at.slot + k] = p[k];
+    m.q[at.grp][at.slot + k] = q[k];
   }
   __syncthreads();
-  const int quarter = threadIdx.x / CH, c = threadIdx.x % CH;
+  constexpr int PER = L::TG / L::PARTS;
+  const int part = threadIdx.x / L::CH, c = threadIdx.x % L::CH;
   float cp = 1.f, cq = 0.f;
 #pragma unroll
-  for (int i = 0; i < TG / 4; ++i) {
-    const int g = quarter * (TG / 4) + (BACK ? TG / 4 - 1 - i : i);
+  for (int i = 0; i < PER; ++i) {
+    const int g = part * PER + (BACK ? PER - 1 - i : i);
     const float gp = m.p[g][c], gq = m.q[g][c];
     m.p[g][c] = cp;
     m.q[g][c] = cq;
     compose(cp, cq, gp, gq);
   }
-  m.tp[quarter][c] = cp;
-  m.tq[quarter][c] = cq;
+  m.tp[part][c] = cp;
+  m.tq[part][c] = cq;
   __syncthreads();
 }
-// What comes into a thread's rows where x comes into the tile.
-template <class T, bool BACK>
-__device__ __forceinline__ float into_group(const Maps<Lay<T>::TG>& m, const Place<T>& at, int k, float x) {
-  constexpr int TG = Lay<T>::TG;
-  const int quarter = at.grp / (TG / 4), c = at.lane * Lay<T>::V + k;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int w = BACK ? 3 - i : i;
-    if (BACK ? w > quarter : w < quarter) x = apply(m.tp[w][c], m.tq[w][c], x);
-  }
-  return apply(m.p[at.grp][c], m.q[at.grp][c], x);
+// What comes into a thread's rows, from what comes into its part of the tile.
+template <class L>
+__device__ __forceinline__ float into_group(const Maps<L>& m, const Place<L>& at, int k, const float (&into)[L::PARTS][L::CH]) {
+  const int c = at.slot + k;
+  return apply(m.p[at.grp][c], m.q[at.grp][c], into[at.grp / (L::TG / L::PARTS)][c]);
 }
-template <class T, bool BACK>
-__device__ __forceinline__ void tile_map(const Maps<Lay<T>::TG>& m, int c, float& p, float& q) {
+// A slot to a lane: what comes into every part where x comes into the tile.
+template <class L, bool BACK>
+__device__ __forceinline__ void into_parts(const Maps<L>& m, int c, float x, float (&into)[L::PARTS][L::CH]) {
+#pragma unroll
+  for (int i = 0; i < L::PARTS; ++i) {
+    const int w = BACK ? L::PARTS - 1 - i : i;
+    into[w][c] = x;
+    x = apply(m.tp[w][c], m.tq[w][c], x);
+  }
+}
+template <class L, bool BACK>
+__device__ __forceinline__ void tile_map(const Maps<L>& m, int c, float& p, float& q) {
   p = 1.f, q = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) compose(p, q, m.tp[BACK ? 3 - i : i][c], m.tq[BACK ? 3 - i : i][c]);
+  for (int i = 0; i < L::PARTS; ++i) compose(p, q, m.tp[BACK ? L::PARTS - 1 - i : i][c], m.tq[BACK ? L::PARTS - 1 - i : i][c]);
 }
 
-// Workspace: the tiles' maps, P and Q, tiles x hidden each; Q's place then holds what comes into each tile.
-__device__ __forceinline__ float* ws_p(const ScanArgs& a) { return (float*)a.workspace; }
-__device__ __forceinline__ float* ws_q(const ScanArgs& a, size_t tiles) { return (float*)a.workspace + tiles * a.hidden; }
+// ------------------------------------------------------------------ the hand-over between tiles
+// Workspace: a ticket counter for every CH features, 64 bytes apart, then a word for every tile and slot, then the rows' flags and
+// sequences, the same for all features.  Counters and words are EMPTY before the kernel; no map has those bits (a NaN is published
+// as the one below).  The tiles of CH features are taken by ticket, in the order in which their states follow each other: a workgroup
+// waits only for tiles that running workgroups have taken, so every wait ends whatever else the GPU does.  (Another call writing the
+// same workspace at the same time would break that: a wait is given up after some seconds, and the states become NaN.)
+constexpr int FAR = 16;    // tiles in front that a wait looks at
+constexpr int AHEAD = 8;   // words on their way together
+constexpr unsigned EMPTY = 0xffffffffu, PUBLISHED_NAN = 0x7fc00000u;
+constexpr long WAIT_TICKS = 500000000;   // of the 100 MHz clock
 
-template <class T, bool TANH, bool WRITE>
-__global__ __launch_bounds__(TPB) void scan_forward_kernel(ScanArgs a, size_t tiles) {
-  typedef Lay<T> L;
-  __shared__ TileRows t;
-  __shared__ Maps<L::TG> m;
-  const long t0 = (long)blockIdx.x * TILE;
-  const size_t c0 = (size_t)blockIdx.y * CH;
-  const Place<T> at(t0, c0, a.hidden);
-  Vec<T> g[L::LS], c[L::LS];
-  load_rows<T>(a.gate, a.gate_stride, at, (long)a.rows, g);
-  load_rows<T>(a.cand, a.cand_stride, at, (long)a.rows, c);
-  size_t s0, s1;
-  tile_rows(a, t0, t, s0, s1);
-  float p[L::LS][L::V], q[L::LS][L::V];
-  row_maps<T, TANH>(a, t, at, g, c, p, q);
-  float gp[L::V], gq[L::V];
-#pragma unroll
-  for (int k = 0; k < L::V; ++k) {
-    gp[k] = 1.f, gq[k] = 0.f;
-#pragma unroll
-    for (int i = 0; i < L::LS; ++i) compose(gp[k], gq[k], p[i][k], q[i][k]);
+__device__ __forceinline__ unsigned long long word_of(float p, float q) {
+  unsigned a = __float_as_uint(p), b = __float_as_uint(q);
+  a = a == EMPTY ? PUBLISHED_NAN : a;
+  b = b == EMPTY ? PUBLISHED_NAN : b;
+  return (unsigned long long)b << 32 | a;
+}
+__device__ __forceinline__ float word_p(unsigned long long w) { return __uint_as_float((unsigned)w); }
+__device__ __forceinline__ float word_q(unsigned long long w) { return __uint_as_float((unsigned)(w >> 32)); }
+__device__ __forceinline__ bool word_there(unsigned long long w) { return (unsigned)w != EMPTY && (unsigned)(w >> 32) != EMPTY; }
+__device__ __forceinline__ bool word_cut(unsigned long long w) { return (unsigned)w == CUT; }
+
+struct Hand {
+  unsigned* tickets;
+  unsigned long long* words;
+  int* seq;
+  unsigned char* flag;
+  size_t tiles, slots;   // slots: the features in whole workgroups
+  static constexpr int MOST_CH = 128;
+  __host__ __device__ static size_t slots_of(size_t hidden) { return (hidden + MOST_CH - 1) / MOST_CH * MOST_CH; }
+  // a ticket counter for every 64 slots, words for all slots
+  __host__ __device__ static size_t clear_bytes(size_t tiles, size_t hidden) { return slots_of(hidden) * (1 + tiles * 8); }
+  __device__ Hand(const ScanArgs& a, size_t tiles_) : tiles(tiles_), slots(slots_of(a.hidden)) {
+    tickets = (unsigned*)a.workspace;
+    words = (unsigned long long*)((char*)a.workspace + slots);
+    seq = (int*)((char*)a.workspace + clear_bytes(tiles, a.hidden));
+    flag = (unsigned char*)(seq + tiles * TILE);
   }
-  scan_groups<T, false>(m, at, gp, gq);
-  if (!WRITE) {
-    const size_t ch = c0 + threadIdx.x;
-    if (threadIdx.x < CH && ch < a.hidden) {
-      float tp, tq;
-      tile_map<T, false>(m, threadIdx.x, tp, tq);
-      ws_p(a)[(size_t)blockIdx.x * a.hidden + ch] = tp;
-      ws_q(a, tiles)[(size_t)blockIdx.x * a.hidden + ch] = tq;
+  __device__ unsigned long long load(size_t tile, size_t ch) const {
+    return __hip_atomic_load(words + tile * slots + ch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ void store(size_t tile, size_t ch, float p, float q) const {
+    __hip_atomic_store(words + tile * slots + ch, word_of(p, q), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+};
+
+// One wave, a slot to a lane: publishes the tile's map, finds what comes into the tile (returned), and publishes what goes out of
+// it.  A wait looks at the words of the tile in front, which are mostly what it needs, and at one word of each of FAR tiles: where the
+// states behind the nearest are not known yet, they are formed from the nearest known ones over the maps between.  (Looking at 64
+// tiles costs every wait 48 lines: 1 .. 3 % where tiles are short of nothing; looking at 8 makes long chains slower, 524,288 x 256
+// bf16 870 us for 731.)
+template <bool BACK>
+__device__ __forceinline__ float hand_over(const Hand& h, size_t order, size_t slot0, float p, float q) {
+  const int lane = threadIdx.x & 63;
+  const size_t slot = slot0 + lane;
+  const auto tile_at = [&](size_t o) { return BACK ? h.tiles - 1 - o : o; };
+  if (order == 0) {
+    h.store(tile_at(0), slot, __uint_as_float(CUT), apply(p, q, 0.f));
+    return 0.f;
+  }
+  h.store(tile_at(order), slot, p, q);
+  const int far = order < FAR ? (int)order : FAR;
+  const long began = wall_clock64();
+  for (;;) {
+    const unsigned long long next = h.load(tile_at(order - 1), slot), s = lane < far ? h.load(tile_at(order - 1 - lane), slot0) : ~0ull;
+    const unsigned long long cuts = __ballot(word_there(s) && word_cut(s)), there = __ballot(word_there(s));
+    int n = cuts ? __ffsll(cuts) : 0;   // tiles to go back to
+    if (n && (~there & ~0ull >> (64 - n))) n = 0;   // (one between is missing)
+    if (__all(word_there(next) && word_cut(next))) n = 1;
+    if (n) {
+      float x = 0.f;
+      bool all = true;
+      for (int at = n; at > 0; at -= AHEAD) {   // from the farthest on, up to AHEAD words on their way together
+        unsigned long long w[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (at - i > 1) w[i] = h.load(tile_at(order - (at - i)), slot);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (at - i > 0) {
+            const unsigned long long v = at - i > 1 ? w[i] : next;
+            all = all && word_there(v) && (at - i < n || word_cut(v));
+            x = apply(word_p(v), word_q(v), x);
+          }
+      }
+      if (__all(all)) {
+        // a tile that cuts the states itself has published what goes out already
+        if (!__all(is_cut(p))) h.store(tile_at(order), slot, __uint_as_float(CUT), apply(p, q, x));
+        return x;
+      }
     }
-    return;
+    if (wall_clock64() - began > WAIT_TICKS) {
+      h.store(tile_at(order), slot, __uint_as_float(CUT), __uint_as_float(PUBLISHED_NAN));
+      return __uint_as_float(PUBLISHED_NAN);
+    }
+    __builtin_amdgcn_s_sleep(2);
   }
-  float h[L::V];
-#pragma unroll
-  for (int k = 0; k < L::V; ++k) h[k] = into_group<T, false>(m, at, k, at.n > k ? ws_q(a, tiles)[(size_t)blockIdx.x * a.hidden + at.ch + k] : 0.f);
+}
+
+// The 64 features of this workgroup: `blocks` consecutive workgroups have one each, every time shifted by one.  Workgroups go to the
+// eight dies in turn; were the features not shifted, a die would read the same few columns of every row, and with them few of its
+// L2's channels (65,536 x 2,048 bf16, forward: 255 us without the shift, 230 with it).
+__device__ __forceinline__ size_t feature_block(size_t blocks) { return (blockIdx.x % blocks + blockIdx.x / blocks) % blocks; }
+
+// Its place in the order of its features' tiles.
+__device__ __forceinline__ size_t take_ticket(const Hand& h, size_t block, unsigned* shared) {
+  if (h.tiles == 1) return 0;
+  if (threadIdx.x == 0)   // the counters start at -1
+    *shared = __hip_atomic_fetch_add(h.tickets + block * 16, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+  __syncthreads();
+  return *shared;
+}
+
+// Sequences without rows hand their state through.
+__device__ __forceinline__ void pass_through(const ScanArgs& a, size_t s0, size_t s1, float* out, const float* from) {
+  for (size_t s = s0; s < s1; ++s) {
+    const long b = a.begin ? bound_at(a.begin, a.index_bytes, s, 0, (long)a.rows) : 0;
+    const long e = a.begin ? bound_at(a.end, a.index_bytes, s, b, (long)a.rows) : (long)a.rows;
+    if (e <= b)
+      for (size_t ch = threadIdx.x; ch < a.hidden; ch += blockDim.x) out[s * a.hidden + ch] = from ? from[s * a.hidden + ch] : 0.f;
+  }
+}
+
+// In front of the scan over several tiles: the rows' flags and sequences (a tile to a workgroup), and the words EMPTY.
+template <bool BACK>
+__global__ __launch_bounds__(TPB) void scan_plan_kernel(ScanArgs a, size_t tiles) {
+  __shared__ TileRows t;
+  const Hand hand(a, tiles);
+  v4u* w = (v4u*)a.workspace;
+  const size_t n16 = Hand::clear_bytes(tiles, a.hidden) / 16;
+  for (size_t i = (size_t)blockIdx.x * TPB + threadIdx.x; i < n16; i += (size_t)gridDim.x * TPB) w[i] = (v4u){EMPTY, EMPTY, EMPTY, EMPTY};
+  for (size_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    size_t s0, s1;
+    tile_rows(a, (long)tile * TILE, t, s0, s1);
+    const int i = threadIdx.x;
+    if (i < TILE) {
+      hand.seq[tile * TILE + i] = t.seq[i];
+      hand.flag[tile * TILE + i] = t.flag[i];
+    }
+    float* out = BACK ? a.dh0 : a.last;
+    if (out) pass_through(a, s0, s1, out, BACK ? a.dlast : a.h0);
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ int rows_of(const ScanArgs& a, size_t tile) {
+  const size_t left = a.rows - tile * TILE;
+  return left < TILE ? (int)left : TILE;
+}
+
+// The rows' flags and sequences of a tile: planned (several tiles), fetched in front of the tile itself and there when it is; or found
+// here.
+struct RowsAhead {
+  int seq;
+  unsigned flag;
+  __device__ RowsAhead(const Hand& hand, size_t tile) {
+    if (hand.tiles > 1) {
+      if (threadIdx.x < TILE) seq = hand.seq[tile * TILE + threadIdx.x];
+      if (threadIdx.x < TILE / 4) flag = ((const unsigned*)hand.flag)[tile * (TILE / 4) + threadIdx.x];
+    }
+  }
+  __device__ void put(const ScanArgs& a, const Hand& hand, TileRows& t, float* out, const float* from) const {
+    if (hand.tiles > 1) {
+      if (threadIdx.x < TILE) t.seq[threadIdx.x] = seq;
+      if (threadIdx.x < TILE / 4) ((unsigned*)t.flag)[threadIdx.x] = flag;
+    } else {
+      size_t s0, s1;
+      tile_rows(a, 0, t, s0, s1);
+      if (blockIdx.x == 0 && out) pass_through(a, s0, s1, out, from);
+    }
+  }
+};
+
+template <bool PLAIN, class L>
+__device__ __forceinline__ void write_forward(const ScanArgs& a, const TileRows& t, const Place<L>& at, size_t tile, const Flags<L>& f,
+                                              const float (&keep)[L::LS][L::V], const float (&zv)[L::LS][L::V], float (&h)[L::V]) {
+  typedef typename L::E T;
+  const TileArray<L, T> out((T*)a.h, a.h_stride, tile, at);
 #pragma unroll
   for (int i = 0; i < L::LS; ++i) {
-    const int r = at.grp * L::LS + i, f = t.flag[r];
+    const bool first = !PLAIN && (f.of(i) & FIRST);
 #pragma unroll
-    for (int k = 0; k < L::V; ++k) h[k] = apply(p[i][k], q[i][k], h[k]);
-    if (a.h && (f & VALID)) store_vec(row_of((T*)a.h, at.row + i, a.h_stride) + (at.n > 0 ? at.ch : 0), pack<T>(h), at.n > 0 ? at.n : 0);
-    if (a.last && (f & LAST))
-#pragma unroll
-      for (int k = 0; k < L::V; ++k)
-        if (k < at.n) a.last[(size_t)t.seq[r] * a.hidden + at.ch + k] = h[k];
-  }
-  if (a.carry && threadIdx.x < CH && c0 + threadIdx.x < a.hidden)
-    a.carry[(size_t)blockIdx.x * a.hidden + c0 + threadIdx.x] = ws_q(a, tiles)[(size_t)blockIdx.x * a.hidden + c0 + threadIdx.x];
-  // sequences without rows keep h0
-  if (a.last && a.last != a.h0)
-    for (size_t s = s0 + threadIdx.x; s < s1; s += TPB) {
-      const long b = a.begin ? bound_at(a.begin, a.index_bytes, s, 0, (long)a.rows) : 0;
-      const long e = a.begin ? bound_at(a.end, a.index_bytes, s, b, (long)a.rows) : (long)a.rows;
-      if (e <= b)
-        for (size_t ch = c0; ch < c0 + CH && ch < a.hidden; ++ch) a.last[s * a.hidden + ch] = a.h0 ? a.h0[s * a.hidden + ch] : 0.f;
+    for (int k = 0; k < L::V; ++k) {
+      const float next = fmaf(keep[i][k], h[k], zv[i][k]);
+      h[k] = first ? zv[i][k] : next;
     }
+    if (a.h && (PLAIN || (f.of(i) & VALID))) store_vec(out.row(i), pack<T>(h), L::NARROW ? at.n : L::V);
+    if (!PLAIN && (f.of(i) & LAST) && a.last) store_state<L>(a.last, t.seq[at.grp * L::LS + i], a, at, h);
+  }
 }
 
-// The tiles' maps in turn, a feature to a lane.
-template <bool BACK>
-__global__ __launch_bounds__(64) void scan_carry_kernel(ScanArgs a, size_t tiles) {
-  const size_t ch = (size_t)blockIdx.x * 64 + threadIdx.x;
-  if (ch >= a.hidden) return;
-  float x = 0.f;
-  for (size_t i = 0; i < tiles; ++i) {
-    const size_t k = (BACK ? tiles - 1 - i : i) * a.hidden + ch;
-    const float p = ws_p(a)[k], q = ws_q(a, tiles)[k];
-    ws_q(a, tiles)[k] = x;
-    x = apply(p, q, x);
+template <class L, bool TANH>
+__global__ __launch_bounds__(TPB, 4) void scan_forward_kernel(ScanArgs a, size_t tiles) {
+  __shared__ TileRows t;
+  __shared__ Maps<L> m;
+  __shared__ __attribute__((aligned(16))) float into[L::PARTS][L::CH];
+  __shared__ unsigned ticket;
+  const Hand hand(a, tiles);
+  const size_t blocks = (a.hidden + L::CH - 1) / L::CH, block = feature_block(blocks), c0 = block * L::CH;
+  const Place<L> at(c0, a.hidden);
+  const size_t order = take_ticket(hand, block, &ticket);
+  const RowsAhead ahead(hand, order);
+  Vec<typename L::E, L::V> g[L::LS], c[L::LS];
+  load_rows<L>(a.gate, a.gate_stride, at, order, rows_of(a, order), g);
+  load_rows<L>(a.cand, a.cand_stride, at, order, rows_of(a, order), c);
+  ahead.put(a, hand, t, a.last, a.h0);
+  float keep[L::LS][L::V], zv[L::LS][L::V];
+#pragma unroll
+  for (int i = 0; i < L::LS; ++i)
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) {
+      float z;
+      gate_of(get(g[i], k), z, keep[i][k]);
+      zv[i][k] = z * (TANH ? tanh_(get(c[i], k)) : get(c[i], k));
+    }
+  __syncthreads();
+  const Flags<L> f(t, at);
+  float p[L::V], q[L::V];
+  if (f.plain) {
+    map_forward<true, L>(f, keep, zv, p, q);
+  } else {
+    if (a.h0) take_in<true, L>(a.h0, FIRST, a, t, at, f, keep, zv);
+    map_forward<false, L>(f, keep, zv, p, q);
   }
+  scan_groups<L, false>(m, at, p, q);
+  if (threadIdx.x < L::CH) {
+    float x = 0.f;
+    if (tiles > 1) {
+      float tp, tq;
+      tile_map<L, false>(m, threadIdx.x, tp, tq);
+      x = hand_over<false>(hand, order, c0, tp, tq);
+    }
+    into_parts<L, false>(m, threadIdx.x, x, into);
+  }
+  __syncthreads();
+  float h[L::V];
+#pragma unroll
+  for (int k = 0; k < L::V; ++k) h[k] = into_group<L>(m, at, k, into);
+  if (a.carry && at.grp == 0) store_state<L>(a.carry, order, a, at, h);
+  if (f.plain)
+    write_forward<true, L>(a, t, at, order, f, keep, zv, h);
+  else
+    write_forward<false, L>(a, t, at, order, f, keep, zv, h);
 }
 
 // Backward: X_t = keep_t G_t is what a row hands to the row in front of it, G_t = d_t + X_{t+1}, d_t = dh_t (+ dlast at a last
 // row); a first row hands it to dh0 and nothing to the row in front, so the cuts are the forward pass's.  h_{t-1} is formed again
-// from the tile's carry in 32 bits: that costs no more than reading the rounded h back, and no rounding.
-template <class T, bool TANH, bool WRITE>
-__global__ __launch_bounds__(TPB) void scan_backward_kernel(ScanArgs a, size_t tiles) {
-  typedef Lay<T> L;
-  __shared__ TileRows t;
-  __shared__ Maps<L::TG> m;
-  const long t0 = (long)blockIdx.x * TILE;
-  const size_t c0 = (size_t)blockIdx.y * CH;
-  const Place<T> at(t0, c0, a.hidden);
-  Vec<T> g[L::LS], c[L::LS], d[L::LS];
-  load_rows<T>(a.gate, a.gate_stride, at, (long)a.rows, g);
-  load_rows<T>(a.cand, a.cand_stride, at, (long)a.rows, c);
-  load_rows<T>(a.dh, a.dh_stride, at, (long)a.rows, d);
-  size_t s0, s1;
-  tile_rows(a, t0, t, s0, s1);
-  float p[L::LS][L::V], q[L::LS][L::V], hp[L::LS][L::V], gp[L::V], gq[L::V];
-  row_maps<T, TANH>(a, t, at, g, c, p, q);
-  if (WRITE) {   // h_{t-1}
+// from the carry in 32 bits: a row less to read than with h, and none of its rounding.
+template <bool PLAIN, class L>
+__device__ __forceinline__ void states_before(const Flags<L>& f, const float (&keep)[L::LS][L::V], float (&x)[L::V], float (&h)[L::LS][L::V]) {
+#pragma unroll
+  for (int i = 0; i < L::LS; ++i)   // h holds z v, and behind this the state in front of the row (at a first row the next pass puts h0)
 #pragma unroll
     for (int k = 0; k < L::V; ++k) {
-      gp[k] = 1.f, gq[k] = 0.f;
-#pragma unroll
-      for (int i = 0; i < L::LS; ++i) compose(gp[k], gq[k], p[i][k], q[i][k]);
+      const float zv = h[i][k], next = fmaf(keep[i][k], x[k], zv);
+      h[i][k] = x[k];
+      x[k] = !PLAIN && (f.of(i) & FIRST) ? zv : next;
     }
-    scan_groups<T, false>(m, at, gp, gq);
-#pragma unroll
-    for (int k = 0; k < L::V; ++k) {
-      float h = into_group<T, false>(m, at, k, k < at.n ? a.carry_in[(size_t)blockIdx.x * a.hidden + at.ch + k] : 0.f);
-#pragma unroll
-      for (int i = 0; i < L::LS; ++i) {
-        const int r = at.grp * L::LS + i;
-        hp[i][k] = (t.flag[r] & FIRST) ? state_at(a.h0, t.seq[r], a.hidden, at.ch + k, at.n - k) : h;
-        h = apply(p[i][k], q[i][k], h);
-      }
-    }
-    __syncthreads();   // the maps are written again below
-  }
-  // the maps of X, and d in q's place
-#pragma unroll
-  for (int k = 0; k < L::V; ++k) {
-    gp[k] = 1.f, gq[k] = 0.f;
-#pragma unroll
-    for (int i = L::LS - 1; i >= 0; --i) {
-      const int r = at.grp * L::LS + i, f = t.flag[r];
-      q[i][k] = get(d[i], k);
-      if (f & LAST) q[i][k] += state_at(a.dlast, t.seq[r], a.hidden, at.ch + k, at.n - k);
-      compose(gp[k], gq[k], p[i][k], is_cut(p[i][k]) ? 0.f : p[i][k] * q[i][k]);
-    }
-  }
-  scan_groups<T, true>(m, at, gp, gq);
-  if (!WRITE) {
-    const size_t ch = c0 + threadIdx.x;
-    if (threadIdx.x < CH && ch < a.hidden) {
-      float tp, tq;
-      tile_map<T, true>(m, threadIdx.x, tp, tq);
-      ws_p(a)[(size_t)blockIdx.x * a.hidden + ch] = tp;
-      ws_q(a, tiles)[(size_t)blockIdx.x * a.hidden + ch] = tq;
-    }
-    return;
-  }
-  float x[L::V];
-#pragma unroll
-  for (int k = 0; k < L::V; ++k) x[k] = into_group<T, true>(m, at, k, k < at.n ? ws_q(a, tiles)[(size_t)blockIdx.x * a.hidden + at.ch + k] : 0.f);
+}
+
+template <bool PLAIN, class L, bool TANH>
+__device__ __forceinline__ void write_back(const ScanArgs& a, const TileRows& t, const Place<L>& at, size_t tile, const Flags<L>& f,
+                                           const float (&keep)[L::LS][L::V], const float (&z)[L::LS][L::V], const float (&v)[L::LS][L::V],
+                                           const float (&h)[L::LS][L::V], const float (&d)[L::LS][L::V], float (&x)[L::V]) {
+  typedef typename L::E T;
+  const TileArray<L, T> out_g((T*)a.dgate, a.dgate_stride, tile, at), out_c((T*)a.dcand, a.dcand_stride, tile, at);
 #pragma unroll
   for (int i = L::LS - 1; i >= 0; --i) {
-    const int r = at.grp * L::LS + i, f = t.flag[r];
-    float og[L::V], oc[L::V], into[L::V];
+    float og[L::V], oc[L::V];
 #pragma unroll
     for (int k = 0; k < L::V; ++k) {
-      float z, keep, v = get(c[i], k);
-      gate_of(get(g[i], k), z, keep);
-      if (TANH) v = tanh_(v);
-      const float G = q[i][k] + x[k];
-      og[k] = G * (z * keep) * (v - hp[i][k]);
-      oc[k] = G * z * (TANH ? fmaf(-v, v, 1.f) : 1.f);
-      into[k] = keep * G;
-      x[k] = is_cut(p[i][k]) ? 0.f : into[k];
+      const float G = d[i][k] + x[k], zG = z[i][k] * G;
+      x[k] = keep[i][k] * G;
+      og[k] = zG * keep[i][k] * (v[i][k] - h[i][k]);
+      oc[k] = TANH ? zG * fmaf(-v[i][k], v[i][k], 1.f) : zG;
     }
-    if (f & VALID) {
-      const long n = at.n > 0 ? at.n : 0;
-      const size_t ch = at.n > 0 ? at.ch : 0;
-      store_vec(row_of((T*)a.dgate, at.row + i, a.dgate_stride) + ch, pack<T>(og), n);
-      store_vec(row_of((T*)a.dcand, at.row + i, a.dcand_stride) + ch, pack<T>(oc), n);
-      if ((f & FIRST) && a.dh0)
+    if (PLAIN || (f.of(i) & VALID)) {
+      store_vec(out_g.row(i), pack<T>(og), L::NARROW ? at.n : L::V);
+      store_vec(out_c.row(i), pack<T>(oc), L::NARROW ? at.n : L::V);
+    }
+    if (!PLAIN && (f.of(i) & FIRST) && a.dh0) store_state<L>(a.dh0, t.seq[at.grp * L::LS + i], a, at, x);
+    if (!PLAIN)
 #pragma unroll
-        for (int k = 0; k < L::V; ++k)
-          if (k < at.n) a.dh0[(size_t)t.seq[r] * a.hidden + at.ch + k] = into[k];
-    }
+      for (int k = 0; k < L::V; ++k) x[k] = (f.of(i) & (FIRST | VALID)) != VALID ? 0.f : x[k];
   }
-  if (a.dh0 && a.dh0 != a.dlast)
-    for (size_t s = s0 + threadIdx.x; s < s1; s += TPB) {
-      const long b = a.begin ? bound_at(a.begin, a.index_bytes, s, 0, (long)a.rows) : 0;
-      const long e = a.begin ? bound_at(a.end, a.index_bytes, s, b, (long)a.rows) : (long)a.rows;
-      if (e <= b)
-        for (size_t ch = c0; ch < c0 + CH && ch < a.hidden; ++ch) a.dh0[s * a.hidden + ch] = a.dlast ? a.dlast[s * a.hidden + ch] : 0.f;
+}
+
+template <class L, bool TANH>
+__global__ __launch_bounds__(TPB, 2) void scan_backward_kernel(ScanArgs a, size_t tiles) {
+  __shared__ TileRows t;
+  __shared__ Maps<L> m, back;
+  __shared__ __attribute__((aligned(16))) float into[L::PARTS][L::CH], before[L::PARTS][L::CH];
+  __shared__ unsigned ticket;
+  const Hand hand(a, tiles);
+  const size_t blocks = (a.hidden + L::CH - 1) / L::CH, block = feature_block(blocks), c0 = block * L::CH;
+  const Place<L> at(c0, a.hidden);
+  const size_t order = take_ticket(hand, block, &ticket), tile = tiles - 1 - order;
+  const RowsAhead ahead(hand, tile);
+  Vec<typename L::E, L::V> g[L::LS], c[L::LS], dh[L::LS];
+  load_rows<L>(a.gate, a.gate_stride, at, tile, rows_of(a, tile), g);
+  load_rows<L>(a.dh, a.dh_stride, at, tile, rows_of(a, tile), dh);
+  load_rows<L>(a.cand, a.cand_stride, at, tile, rows_of(a, tile), c);
+  ahead.put(a, hand, t, a.dh0, a.dlast);
+  float keep[L::LS][L::V], z[L::LS][L::V], v[L::LS][L::V], d[L::LS][L::V], h[L::LS][L::V];
+#pragma unroll
+  for (int i = 0; i < L::LS; ++i) {
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) {
+      gate_of(get(g[i], k), z[i][k], keep[i][k]);
+      d[i][k] = get(dh[i], k);
+      v[i][k] = TANH ? tanh_(get(c[i], k)) : get(c[i], k);
+      h[i][k] = z[i][k] * v[i][k];
     }
+    // a row's tangents are formed here: moved behind the barrier, all of them side by side do not fit the registers
+    if (TANH)
+#pragma unroll
+      for (int k = 0; k < L::V; ++k) asm volatile("" : "+v"(v[i][k]));
+  }
+  __syncthreads();
+  const Flags<L> f(t, at);
+  float p[L::V], q[L::V], x[L::V];
+  if (f.plain) {
+    map_back<true, L>(f, keep, d, p, q);
+  } else {
+    if (a.dlast) take_in<false, L>(a.dlast, LAST, a, t, at, f, keep, d);
+    map_back<false, L>(f, keep, d, p, q);
+  }
+  scan_groups<L, true>(back, at, p, q);
+  if (f.plain) {
+    map_forward<true, L>(f, keep, h, p, q);
+  } else {
+    if (a.h0) take_in<true, L>(a.h0, FIRST, a, t, at, f, keep, h);
+    map_forward<false, L>(f, keep, h, p, q);
+  }
+  scan_groups<L, false>(m, at, p, q);
+  if (threadIdx.x < L::CH) {
+    float in = 0.f;
+    if (tiles > 1) {
+      float tp, tq;
+      tile_map<L, true>(back, threadIdx.x, tp, tq);
+      in = hand_over<true>(hand, order, c0, tp, tq);
+    }
+    into_parts<L, true>(back, threadIdx.x, in, into);
+  } else if (threadIdx.x < 2 * L::CH) {   // beside it
+    const int s = threadIdx.x - L::CH;
+    const bool in = !L::NARROW || (size_t)s < a.hidden;
+    into_parts<L, false>(m, s, in ? a.carry_in[tile * a.hidden + feature_of<L>(s, c0, a.hidden)] : 0.f, before);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < L::V; ++k) x[k] = into_group<L>(m, at, k, before);
+  if (f.plain) {
+    states_before<true, L>(f, keep, x, h);
+  } else {
+    states_before<false, L>(f, keep, x, h);
+#pragma unroll
+    for (int i = 0; i < L::LS; ++i)
+      if (f.of(i) & FIRST)
+#pragma unroll
+        for (int k = 0; k < L::V; ++k) h[i][k] = 0.f;
+    if (a.h0) take_in<false, L>(a.h0, FIRST, a, t, at, f, keep, h);
+  }
+#pragma unroll
+  for (int k = 0; k < L::V; ++k) x[k] = into_group<L>(back, at, k, into);
+  if (f.plain)
+    write_back<true, L, TANH>(a, t, at, tile, f, keep, z, v, h, d, x);
+  else
+    write_back<false, L, TANH>(a, t, at, tile, f, keep, z, v, h, d, x);
 }
 
 // One row of every sequence: bound by the call itself.  A group of 16 bytes of the inputs to a lane.
@@ -419,37 +720,45 @@ __global__ __launch_bounds__(TPB) void scan_step_kernel(ScanStepArgs a) {
 }
 
 size_t tiles_of(size_t rows) { return rows ? (rows + TILE - 1) / TILE : 1; }   // sequences without rows have a tile too
+size_t bytes_of(size_t tiles, size_t hidden) {
+  return tiles == 1 ? 0 : (Hand::clear_bytes(tiles, hidden) + tiles * TILE * 5 + 15) / 16 * 16;
+}
+
+template <class L, bool BACK>
+hipError_t run(void (*kernel)(ScanArgs, size_t), const ScanArgs* a, hipStream_t stream) {
+  const size_t tiles = tiles_of(a->rows), blocks = (a->hidden + L::CH - 1) / L::CH;
+  if (tiles > 1) {
+    const hipError_t e = launch(scan_plan_kernel<BACK>, dim3((unsigned)(tiles < 1024 ? tiles : 1024)), dim3(TPB), 0, stream, *a, tiles);
+    if (e != hipSuccess) return e;
+  }
+  return launch(kernel, dim3((unsigned)(blocks * tiles)), dim3(TPB), 0, stream, *a, tiles);
+}
 
 }  // namespace
 
 extern "C" size_t amp_scan_carry_rows(int, size_t rows, size_t) { return tiles_of(rows); }
-extern "C" size_t amp_scan_workspace_bytes(int, size_t rows, size_t hidden) { return (tiles_of(rows) * hidden * 8 + 15) / 16 * 16; }
+extern "C" size_t amp_scan_workspace_bytes(int, size_t rows, size_t hidden) { return bytes_of(tiles_of(rows), hidden); }
 
-#define BY_TANH(K, ...)                                                        \
-  if (tanh) {                                                                  \
-    if ((e = launch(K<T, true __VA_OPT__(, ) __VA_ARGS__>, grid, dim3(TPB), 0, stream, *a, tiles)) != hipSuccess) return e;  \
-  } else {                                                                     \
-    if ((e = launch(K<T, false __VA_OPT__(, ) __VA_ARGS__>, grid, dim3(TPB), 0, stream, *a, tiles)) != hipSuccess) return e; \
-  }
+namespace {
+template <class T, bool NARROW>
+hipError_t forward(int tanh, const ScanArgs* a, hipStream_t stream) {
+  typedef Lay<T, NARROW> L;
+  return run<L, false>(tanh ? scan_forward_kernel<L, true> : scan_forward_kernel<L, false>, a, stream);
+}
+template <class T, bool NARROW>
+hipError_t backward(int tanh, const ScanArgs* a, hipStream_t stream) {
+  typedef Lay<T, NARROW> L;
+  return run<L, true>(tanh ? scan_backward_kernel<L, true> : scan_backward_kernel<L, false>, a, stream);
+}
+
+}  // namespace
 
 extern "C" hipError_t amp_scan_forward_launch(int dtype, int tanh, const ScanArgs* a, hipStream_t stream) {
-  const size_t tiles = tiles_of(a->rows);
-  const dim3 grid((unsigned)tiles, (unsigned)((a->hidden + CH - 1) / CH));
-  hipError_t e;
-  OPS_BY_TYPE(dtype, BY_TANH(scan_forward_kernel, false));
-  if ((e = launch(scan_carry_kernel<false>, dim3((unsigned)((a->hidden + 63) / 64)), dim3(64), 0, stream, *a, tiles)) != hipSuccess) return e;
-  OPS_BY_TYPE(dtype, BY_TANH(scan_forward_kernel, true));
-  return hipSuccess;
+  OPS_BY_TYPE(dtype, return a->hidden < Lay<T, false>::V ? forward<T, true>(tanh, a, stream) : forward<T, false>(tanh, a, stream));
 }
 
 extern "C" hipError_t amp_scan_backward_launch(int dtype, int tanh, const ScanArgs* a, hipStream_t stream) {
-  const size_t tiles = tiles_of(a->rows);
-  const dim3 grid((unsigned)tiles, (unsigned)((a->hidden + CH - 1) / CH));
-  hipError_t e;
-  OPS_BY_TYPE(dtype, BY_TANH(scan_backward_kernel, false));
-  if ((e = launch(scan_carry_kernel<true>, dim3((unsigned)((a->hidden + 63) / 64)), dim3(64), 0, stream, *a, tiles)) != hipSuccess) return e;
-  OPS_BY_TYPE(dtype, BY_TANH(scan_backward_kernel, true));
-  return hipSuccess;
+  OPS_BY_TYPE(dtype, return a->hidden < Lay<T, false>::V ? backward<T, true>(tanh, a, stream) : backward<T, false>(tanh, a, stream));
 }
 
 extern "C" hipError_t amp_scan_step_launch(int dtype, int tanh, const ScanStepArgs* a, hipStream_t stream) {
