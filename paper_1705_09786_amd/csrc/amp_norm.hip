@@ -7,7 +7,7 @@
 
 namespace {
 
-constexpr int TPB = 256, NW = TPB / 64;
+constexpr int TPB = 256;
 
 // Where a thread's groups of a row lie.  TPR threads share a row, thread l has the groups l, l + TPR, ...; the row's last group, where it
 // would pass the row's end, is moved back to end with it, and the elements that the group in front of it has as well do not count
@@ -74,14 +74,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_forward_kernel(Nor
       }
   const float inv = 1.f / (float)a.cols;
   const size_t step = (size_t)gridDim.x * RPW;
+  Vec<T> ahead[NV];   // the next row, on its way while this one is worked on
+  const auto fetch = [&](size_t r0) {
+    const size_t r = r0 + threadIdx.x / TPR;
+    const T* x = row_of((const T*)a.x, r < a.rows ? r : a.rows - 1, a.x_stride);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j <= R.last) ahead[j] = R.load(x, j);
+  };
+  fetch((size_t)blockIdx.x * RPW);
   for (size_t r0 = (size_t)blockIdx.x * RPW; r0 < a.rows; r0 += step) {
     const size_t r = r0 + threadIdx.x / TPR;
     const bool in = r < a.rows;
-    const T* x = row_of((const T*)a.x, in ? r : a.rows - 1, a.x_stride);
     Vec<T> v[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j <= R.last) v[j] = R.load(x, j);
+    for (int j = 0; j < NV; ++j) v[j] = ahead[j];
+    if (r0 + step < a.rows) fetch(r0 + step);
     float s[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -139,20 +147,30 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
     }
   const float inv = 1.f / (float)a.cols;
   const size_t step = (size_t)gridDim.x * RPW;
+  constexpr bool AHEAD = TPR * NV <= 2048;   // longer rows leave no registers for a second one
+  Vec<T> ahead_x[NV], ahead_dy[NV];          // the next row, on its way while this one is worked on
+  float ahead_mean, ahead_rstd;
+  const auto fetch = [&](size_t r0) {
+    const size_t r = r0 + threadIdx.x / TPR, rr = r < a.rows ? r : a.rows - 1;
+    const T *x = row_of((const T*)a.x, rr, a.x_stride), *dy = row_of((const T*)a.dy, rr, a.dy_stride);
+    ahead_mean = a.mean[rr], ahead_rstd = a.rstd[rr];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j <= R.last) {
+        ahead_x[j] = R.load(x, j);
+        ahead_dy[j] = R.load(dy, j);
+      }
+  };
+  fetch((size_t)blockIdx.x * RPW);
   int turn = 0;
   for (size_t r0 = (size_t)blockIdx.x * RPW; r0 < a.rows; r0 += step, turn ^= 1) {
     const size_t r = r0 + threadIdx.x / TPR;
     const bool in = r < a.rows;
-    const size_t rr = in ? r : a.rows - 1;
-    const T *x = row_of((const T*)a.x, rr, a.x_stride), *dy = row_of((const T*)a.dy, rr, a.dy_stride);
     Vec<T> v[NV], g[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j <= R.last) {
-        v[j] = R.load(x, j);
-        g[j] = R.load(dy, j);
-      }
-    const float mean = a.mean[rr], rstd = a.rstd[rr];
+    for (int j = 0; j < NV; ++j) v[j] = ahead_x[j], g[j] = ahead_dy[j];
+    const float mean = ahead_mean, rstd = ahead_rstd;
+    if (AHEAD && r0 + step < a.rows) fetch(r0 + step);
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -185,6 +203,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
           }
       }
     }
+    if (!AHEAD && r0 + step < a.rows) fetch(r0 + step);
   }
   if (!a.dweight && !a.dbias) return;
   // the rows that the workgroup's waves have side by side are joined first, in their order
@@ -230,36 +249,37 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
 }
 
 // Longer rows than the registers hold: one workgroup a row at a time, read again for each of mean, deviations and result.
+constexpr int LONG = 1024;
 template <class T>
-__global__ __launch_bounds__(TPB) void norm_forward_long_kernel(NormArgs a) {
+__global__ __launch_bounds__(LONG) void norm_forward_long_kernel(NormArgs a) {
   constexpr int N = Vec<T>::N;
-  __shared__ float part[2][NW][1];
+  __shared__ float part[2][LONG / 64][1];
   const long cols = (long)a.cols;
   for (size_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* x = row_of((const T*)a.x, r, a.x_stride);
     T* y = row_of((T*)a.y, r, a.y_stride);
     float s[1] = {0.f};
-    for (long c = threadIdx.x * N; c < cols; c += TPB * N) {
+    for (long c = threadIdx.x * N; c < cols; c += LONG * N) {
       const Vec<T> v = load_vec(x + c, cols - c);
 #pragma unroll
       for (int k = 0; k < N; ++k) s[0] += get(v, k);
     }
-    block_sum<NW>(s, part[0]);
+    block_sum<LONG / 64>(s, part[0]);
     const float mean = s[0] / (float)cols;
     float q[1] = {0.f};
-    for (long c = threadIdx.x * N; c < cols; c += TPB * N) {
+    for (long c = threadIdx.x * N; c < cols; c += LONG * N) {
       const Vec<T> v = load_vec(x + c, cols - c);
 #pragma unroll
       for (int k = 0; k < N; ++k)
         if (c + k < cols) q[0] = fmaf(get(v, k) - mean, get(v, k) - mean, q[0]);
     }
-    block_sum<NW>(q, part[1]);
+    block_sum<LONG / 64>(q, part[1]);
     const float rstd = 1.f / sqrtf(q[0] / (float)cols + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
-    for (long c = threadIdx.x * N; c < cols; c += TPB * N) {
+    for (long c = threadIdx.x * N; c < cols; c += LONG * N) {
       const Vec<T> v = load_vec(x + c, cols - c);
       float o[N];
 #pragma unroll
@@ -273,9 +293,9 @@ __global__ __launch_bounds__(TPB) void norm_forward_long_kernel(NormArgs a) {
 }
 
 template <class T>
-__global__ __launch_bounds__(TPB) void norm_dx_long_kernel(NormArgs a) {
+__global__ __launch_bounds__(LONG) void norm_dx_long_kernel(NormArgs a) {
   constexpr int N = Vec<T>::N;
-  __shared__ float part[2][NW][2];
+  __shared__ float part[2][LONG / 64][2];
   const long cols = (long)a.cols;
   int turn = 0;
   for (size_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
@@ -284,7 +304,7 @@ __global__ __launch_bounds__(TPB) void norm_dx_long_kernel(NormArgs a) {
     T* dx = row_of((T*)a.dx, r, a.dx_stride);
     const float mean = a.mean[r], rstd = a.rstd[r];
     float s[2] = {0.f, 0.f};
-    for (long c = threadIdx.x * N; c < cols; c += TPB * N) {
+    for (long c = threadIdx.x * N; c < cols; c += LONG * N) {
       const Vec<T> v = load_vec(x + c, cols - c), g = load_vec(dy + c, cols - c);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
@@ -293,9 +313,9 @@ __global__ __launch_bounds__(TPB) void norm_dx_long_kernel(NormArgs a) {
         if (c + k < cols) s[1] = fmaf(q, (get(v, k) - mean) * rstd, s[1]);
       }
     }
-    block_sum<NW>(s, part[turn]);
+    block_sum<LONG / 64>(s, part[turn]);
     const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
-    for (long c = threadIdx.x * N; c < cols; c += TPB * N) {
+    for (long c = threadIdx.x * N; c < cols; c += LONG * N) {
       const Vec<T> v = load_vec(x + c, cols - c), g = load_vec(dy + c, cols - c);
       float o[N];
 #pragma unroll
@@ -342,20 +362,11 @@ __global__ __launch_bounds__(32 * JOIN) void norm_join_kernel(NormArgs a, int pa
   }
 }
 
-#ifndef FEW
-#define FEW 512
-#endif
-#ifndef PARTS1024
-#define PARTS1024 256
-#endif
-#ifndef PARTS256
-#define PARTS256 512
-#endif
-#ifndef GRIDF
-#define GRIDF 2048
-#endif
-// Which kernel takes a row: the threads that share it and the 16-byte groups of each.  A wave to a row of up to 256 groups (no
-// barriers), more threads beyond and for few rows, whose call is a latency.
+// Which kernel takes a row: the threads that share it and the 16-byte groups of each.  A wave to a row of up to 128 groups (256
+// forward) has no barriers; longer rows, and rows so few that a call is a latency (512 and fewer), have more threads.  The backward pass
+// keeps three values a column beside the row, so its threads have fewer groups: 2,500 x 11,111 fp16 takes 70 us on 1,024 threads of
+// two, 61 on 512 of four (forward 33 and 38).  Its workgroups, of which each leaves a part of the parameters' gradients to be read
+// again, have at least eight rows: 512 x 4,096 bf16 takes 27 us with a row to each, 2,048 x 4,096 43 us and 27 with eight.
 struct Shape {
   int tpr, nv, parts;   // tpr = 0: longer than the registers hold; parts: workgroups of the backward pass
 };
@@ -364,16 +375,15 @@ Shape shape_of(int dtype, size_t rows, size_t cols, bool backward) {
   Shape s = {0, 0, 0};
   if (groups <= 16) s = {16, 1, 0};
   else if (groups <= 64) s = {64, 1, 0};
-  else if (groups <= 256 && rows <= FEW) s = {256, 1, 0};
+  else if (groups <= 256 && (backward ? groups > 128 || rows <= 512 : rows <= 512)) s = {256, 1, 0};
   else if (groups <= 128) s = {64, 2, 0};
-  else if (groups <= 256 && !backward) s = {64, 4, 0};
-  else if (groups <= 256) s = {256, 1, 0};
+  else if (groups <= 256) s = {64, 4, 0};
   else if (groups <= 512) s = {256, 2, 0};
-  else if (groups <= 1024) s = {backward ? 1024 : 256, backward ? 1 : 4, 0};
-  else if (groups <= 2048) s = {1024, 2, 0};
-  else if (groups <= 4096 && !backward) s = {1024, 4, 0};
-  const size_t rpw = s.tpr == 0 ? 1 : s.tpr > 256 ? 1 : 256 / s.tpr, most = s.tpr == 0 ? 64 : s.tpr > 256 ? PARTS1024 : PARTS256;
-  const size_t need = (rows + rpw - 1) / rpw;
+  else if (groups <= 1024) s = backward ? Shape{1024, 1, 0} : Shape{256, 4, 0};
+  else if (groups <= 2048) s = backward ? Shape{512, 4, 0} : Shape{1024, 2, 0};
+  else if (groups <= 4096 && (!backward || dtype == 0)) s = {1024, 4, 0};
+  const size_t rpw = s.tpr && s.tpr < 256 ? 256 / s.tpr : 1, most = s.tpr == 0 ? 64 : s.tpr > 256 ? 256 : 512;
+  const size_t need = (rows + rpw * 8 - 1) / (rpw * 8);
   s.parts = (int)(need < most ? need : most);
   return s;
 }
@@ -384,19 +394,19 @@ Shape shape_of(int dtype, size_t rows, size_t cols, bool backward) {
     case 64 * 8 + 1: return K(64, 1);                    \
     case 64 * 8 + 2: return K(64, 2);                    \
     case 256 * 8 + 1: return K(256, 1);                  \
-    case 256 * 8 + 2: return K(256, 2);                  \
-    case 1024 * 8 + 2: return K(1024, 2);
+    case 256 * 8 + 2: return K(256, 2);
 
 template <class T>
 hipError_t forward(const Shape& s, const NormArgs* a, hipStream_t stream) {
   const size_t rpw = s.tpr && s.tpr < 256 ? 256 / s.tpr : 1, need = (a->rows + rpw - 1) / rpw;
 #define NORM_F(TPR, NV) \
-  launch(norm_forward_kernel<T, TPR, NV>, dim3((unsigned)(need < GRIDF ? need : GRIDF)), dim3(TPR > 256 ? TPR : 256), 0, stream, *a)
+  launch(norm_forward_kernel<T, TPR, NV>, dim3((unsigned)(need < 768 ? need : 768)), dim3(TPR > 256 ? TPR : 256), 0, stream, *a)
   NORM_SHAPES(NORM_F)
     case 64 * 8 + 4: return NORM_F(64, 4);
     case 256 * 8 + 4: return NORM_F(256, 4);
+    case 1024 * 8 + 2: return NORM_F(1024, 2);
     case 1024 * 8 + 4: return NORM_F(1024, 4);
-    default: return launch(norm_forward_long_kernel<T>, dim3((unsigned)(a->rows < 4096 ? a->rows : 4096)), dim3(TPB), 0, stream, *a);
+    default: return launch(norm_forward_long_kernel<T>, dim3((unsigned)(a->rows < 4096 ? a->rows : 4096)), dim3(LONG), 0, stream, *a);
   }
 }
 
@@ -404,14 +414,17 @@ template <class T>
 hipError_t backward(const Shape& s, const NormArgs* a, hipStream_t stream) {
 #define NORM_B(TPR, NV) launch(norm_backward_kernel<T, TPR, NV>, dim3((unsigned)s.parts), dim3(TPR > 256 ? TPR : 256), 0, stream, *a)
   NORM_SHAPES(NORM_B)
+    case 512 * 8 + 4: return NORM_B(512, 4);
     case 1024 * 8 + 1: return NORM_B(1024, 1);
     default: break;
   }
+  if constexpr (sizeof(T) == 4)
+    if (s.tpr == 1024 && s.nv == 4) return NORM_B(1024, 4);
   if (a->dweight || a->dbias) {   // before dx, which may take dy's or x's place
     const hipError_t e = launch(norm_dw_long_kernel<T>, dim3((unsigned)((a->cols + TPB - 1) / TPB), (unsigned)s.parts), dim3(TPB), 0, stream, *a, s.parts);
     if (e != hipSuccess || !a->dx) return e;
   }
-  return launch(norm_dx_long_kernel<T>, dim3((unsigned)(a->rows < 4096 ? a->rows : 4096)), dim3(TPB), 0, stream, *a);
+  return launch(norm_dx_long_kernel<T>, dim3((unsigned)(a->rows < 4096 ? a->rows : 4096)), dim3(LONG), 0, stream, *a);
 }
 
 }  // namespace

@@ -20,6 +20,12 @@ ACTIVATIONS = {"none": B.ACT_NONE, "tanh": B.ACT_TANH}
 _INDEX = {torch.int32: 4, torch.int64: 8}
 
 
+# A small call is bound by what it does on the host, so torch's own current device and stream are read without its Python layer
+# where this torch has them (0.2 us for 1.7).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _refuse(msg):
     raise B.AmpError(B.AMP_EINVAL, msg)
 
@@ -29,52 +35,52 @@ def _check(rc):
         raise B.AmpError(rc, B.lib().amp_operator_error().decode())
 
 
+def _call(x, name, *args):
+    """A C call on the current stream of x's device, which is current during the call."""
+    index, fn = x.get_device(), getattr(B.lib(), name)
+    if index == _current_device():
+        rc = fn(*args, _stream_of(index))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream_of(index))
+    if rc:
+        _check(rc)
+
+
 def _rows(name, x, like=None, dtypes=DTYPES, shape=None):
-    """x as rows of consecutive elements: (its address, its row stride); `like`: a tensor whose device it has to be on."""
+    """x as rows of consecutive elements: (its address, its row stride); `like`: a tensor whose device (and, for arrays of the operators'
+    types, type) it has to share."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         _refuse("%s is not a 2-D tensor" % name)
     if not x.is_cuda:
         _refuse("%s is not on a GPU" % name)
     if x.dtype not in dtypes:
         _refuse("%s is of type %s" % (name, x.dtype))
-    if like is not None and x.device != like.device:
-        _refuse("%s is on another device" % name)
-    if shape is not None and tuple(x.shape) != shape:
-        _refuse("%s is %s, %s is needed" % (name, tuple(x.shape), shape))
-    if x.size(1) > 1 and x.stride(1) != 1:
+    if like is not None:
+        if x.get_device() != like.get_device():
+            _refuse("%s is on another device" % name)
+        if dtypes is DTYPES and x.dtype != like.dtype:
+            _refuse("%s is of type %s, not %s" % (name, x.dtype, like.dtype))
+    if shape is not None and x.shape != shape:
+        _refuse("%s is %s, %s is needed" % (name, tuple(x.shape), tuple(shape)))
+    row, col = x.stride()
+    if col != 1 and x.size(1) > 1:
         _refuse("%s does not have its features next to each other (call contiguous())" % name)
-    return x.data_ptr(), x.stride(0)
+    return x.data_ptr(), row
 
 
 def _floats(name, x, like, *shape):
     """A contiguous float32 tensor of that shape, or None: its address."""
     if x is None:
         return None
-    if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or tuple(x.shape) != shape or not x.is_contiguous() or x.device != like.device:
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.device != like.device:
         _refuse("%s is not a contiguous float32 tensor of shape %s on %s" % (name, shape, like.device))
     return x.data_ptr()
 
 
-def _same_type(name, x, like):
-    if x.dtype != like.dtype:
-        _refuse("%s is of type %s, not %s" % (name, x.dtype, like.dtype))
-
-
-class _On:
-    """The tensors' device made current for a call, and its stream's handle."""
-
-    def __init__(self, x):
-        self.index = x.device.index
-        self.before = torch.cuda.current_device()
-
-    def __enter__(self):
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *_):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+def _new(x):
+    """An array of x's shape and type."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 @lru_cache(maxsize=4096)
@@ -98,16 +104,14 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, stats=False, out=None):
     """(x - mean) / sqrt(var + eps) * weight + bias over each row, in x's type; with stats also the rows' mean and 1 / sqrt(var + eps),
     which the backward pass needs: (y, mean, rstd).  out: a tensor to write to (may be x)."""
     px, sx = _rows("x", x)
-    rows, cols = x.shape
-    y = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out
-    py, sy = _rows("out", y, x, shape=(rows, cols))
-    _same_type("out", y, x)
+    rows, cols = shape = x.shape
+    y = _new(x) if out is None else out
+    py, sy = _rows("out", y, x, shape=shape)
+    pw, pb = _floats("weight", weight, x, cols), _floats("bias", bias, x, cols)
     mean = rstd = None
     if stats:
         mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    with _On(x) as stream:
-        _check(B.lib().amp_layer_norm_forward(DTYPES[x.dtype], rows, cols, px, sx, _floats("weight", weight, x, cols),
-                                              _floats("bias", bias, x, cols), eps, py, sy, _ptr(mean), _ptr(rstd), stream))
+    _call(x, "amp_layer_norm_forward", DTYPES[x.dtype], rows, cols, px, sx, pw, pb, eps, py, sy, _ptr(mean), _ptr(rstd))
     return (y, mean, rstd) if stats else y
 
 
@@ -115,20 +119,17 @@ def layer_norm_backward(dy, x, weight, mean, rstd, *, out=None):
     """(dx, dweight, dbias) from the gradient of y, x, the weight (or None) and the statistics of layer_norm(.., stats=True).
     out: a tensor for dx (may be dy or x)."""
     px, sx = _rows("x", x)
-    rows, cols = x.shape
-    pd, sd = _rows("dy", dy, x, shape=(rows, cols))
-    _same_type("dy", dy, x)
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out
-    po, so = _rows("out", dx, x, shape=(rows, cols))
-    _same_type("out", dx, x)
+    rows, cols = shape = x.shape
+    pd, sd = _rows("dy", dy, x, shape=shape)
+    dx = _new(x) if out is None else out
+    po, so = _rows("out", dx, x, shape=shape)
     if mean is None or rstd is None:
         _refuse("mean and rstd are needed")
-    pm, pr = _floats("mean", mean, x, rows), _floats("rstd", rstd, x, rows)
+    pm, pr, pw = _floats("mean", mean, x, rows), _floats("rstd", rstd, x, rows), _floats("weight", weight, x, cols)
     dweight, dbias = torch.empty((2, cols), dtype=torch.float32, device=x.device)
-    with _On(x) as stream:
-        ws, n = _workspace("amp_layer_norm_workspace", x)
-        _check(B.lib().amp_layer_norm_backward(DTYPES[x.dtype], rows, cols, pd, sd, px, sx, _floats("weight", weight, x, cols), pm, pr,
-                                               po, so, dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), n, stream))
+    ws, n = _workspace("amp_layer_norm_workspace", x)
+    _call(x, "amp_layer_norm_backward", DTYPES[x.dtype], rows, cols, pd, sd, px, sx, pw, pm, pr, po, so, dweight.data_ptr(), dbias.data_ptr(),
+          _ptr(ws), n)
     return dx, dweight, dbias
 
 
@@ -170,22 +171,18 @@ def gated_scan(gate, cand, sequences=None, *, h0=None, activation="none", last=F
     float32, None = zeros.  last=True: the states behind the last rows, (n, features) float32, else None.  carry=True: what
     gated_scan_backward starts from, else None."""
     pg, sg = _rows("gate", gate)
-    rows, hidden = gate.shape
-    pc, sc = _rows("cand", cand, gate, shape=(rows, hidden))
-    _same_type("cand", cand, gate)
+    rows, hidden = shape = gate.shape
+    pc, sc = _rows("cand", cand, gate, shape=shape)
     act = _activation(activation)
     seq, n = _sequences(sequences, gate)
-    h = torch.empty((rows, hidden), dtype=gate.dtype, device=gate.device) if out is None else out
-    ph, sh = _rows("out", h, gate, shape=(rows, hidden))
-    _same_type("out", h, gate)
+    h = _new(gate) if out is None else out
+    ph, sh = _rows("out", h, gate, shape=shape)
     p0 = _floats("h0", h0, gate, n, hidden)
     dtype = DTYPES[gate.dtype]
     end = torch.empty((n, hidden), dtype=torch.float32, device=gate.device) if last else None
     car = torch.empty((_size("amp_gated_scan_carry", dtype, rows, hidden), hidden), dtype=torch.float32, device=gate.device) if carry else None
-    with _On(gate) as stream:
-        ws, nb = _workspace("amp_gated_scan_workspace", gate)
-        _check(B.lib().amp_gated_scan_forward(dtype, act, rows, hidden, pg, sg, pc, sc, ct.byref(seq), p0, ph, sh, _ptr(end), _ptr(car),
-                                              _ptr(ws), nb, stream))
+    ws, nb = _workspace("amp_gated_scan_workspace", gate)
+    _call(gate, "amp_gated_scan_forward", dtype, act, rows, hidden, pg, sg, pc, sc, ct.byref(seq), p0, ph, sh, _ptr(end), _ptr(car), _ptr(ws), nb)
     return h, end, car
 
 
@@ -193,44 +190,39 @@ def gated_scan_backward(dh, gate, cand, carry, sequences=None, *, h0=None, dlast
     """(dgate, dcand, dh0) from the gradient of h (and of last: dlast), the inputs and the carry of
     gated_scan(.., carry=True).  out: a pair of tensors for dgate and dcand."""
     pg, sg = _rows("gate", gate)
-    rows, hidden = gate.shape
-    pc, sc = _rows("cand", cand, gate, shape=(rows, hidden))
-    pd, sd = _rows("dh", dh, gate, shape=(rows, hidden))
-    _same_type("cand", cand, gate)
-    _same_type("dh", dh, gate)
+    rows, hidden = shape = gate.shape
+    pc, sc = _rows("cand", cand, gate, shape=shape)
+    pd, sd = _rows("dh", dh, gate, shape=shape)
     act = _activation(activation)
     seq, n = _sequences(sequences, gate)
-    dgate, dcand = out if out is not None else (torch.empty((rows, hidden), dtype=gate.dtype, device=gate.device) for _ in range(2))
-    po, so = _rows("dgate", dgate, gate, shape=(rows, hidden))
-    pq, sq = _rows("dcand", dcand, gate, shape=(rows, hidden))
-    _same_type("dgate", dgate, gate)
-    _same_type("dcand", dcand, gate)
+    dgate, dcand = out if out is not None else (_new(gate), _new(gate))
+    po, so = _rows("dgate", dgate, gate, shape=shape)
+    pq, sq = _rows("dcand", dcand, gate, shape=shape)
     dtype = DTYPES[gate.dtype]
     if carry is None:
         _refuse("carry is needed")
     pk = _floats("carry", carry, gate, _size("amp_gated_scan_carry", dtype, rows, hidden), hidden)
     p0, pl = _floats("h0", h0, gate, n, hidden), _floats("dlast", dlast, gate, n, hidden)
     dh0 = torch.empty((n, hidden), dtype=torch.float32, device=gate.device)
-    with _On(gate) as stream:
-        ws, nb = _workspace("amp_gated_scan_workspace", gate)
-        _check(B.lib().amp_gated_scan_backward(dtype, act, rows, hidden, pd, sd, pl, pg, sg, pc, sc, ct.byref(seq), p0, pk, po, so, pq, sq,
-                                               dh0.data_ptr(), _ptr(ws), nb, stream))
+    ws, nb = _workspace("amp_gated_scan_workspace", gate)
+    _call(gate, "amp_gated_scan_backward", dtype, act, rows, hidden, pd, sd, pl, pg, sg, pc, sc, ct.byref(seq), p0, pk, po, so, pq, sq,
+          dh0.data_ptr(), _ptr(ws), nb)
     return dgate, dcand, dh0
+
+
+_FLOAT_ROWS = (torch.float32,)
 
 
 def gated_scan_step(gate, cand, state, *, activation="none", out=None):
     """One row of every sequence: state (rows, features; float32, features next to each other) becomes
     (1 - z) state + z act(cand), in place; returns h, its rounded copy."""
     pg, sg = _rows("gate", gate)
-    rows, hidden = gate.shape
-    pc, sc = _rows("cand", cand, gate, shape=(rows, hidden))
-    _same_type("cand", cand, gate)
-    ps, ss = _rows("state", state, gate, dtypes=(torch.float32,), shape=(rows, hidden))
-    h = torch.empty((rows, hidden), dtype=gate.dtype, device=gate.device) if out is None else out
-    ph, sh = _rows("out", h, gate, shape=(rows, hidden))
-    _same_type("out", h, gate)
-    with _On(gate) as stream:
-        _check(B.lib().amp_gated_scan_step(DTYPES[gate.dtype], _activation(activation), rows, hidden, pg, sg, pc, sc, ps, ss, ph, sh, stream))
+    rows, hidden = shape = gate.shape
+    pc, sc = _rows("cand", cand, gate, shape=shape)
+    ps, ss = _rows("state", state, gate, _FLOAT_ROWS, shape)
+    h = _new(gate) if out is None else out
+    ph, sh = _rows("out", h, gate, shape=shape)
+    _call(gate, "amp_gated_scan_step", DTYPES[gate.dtype], _activation(activation), rows, hidden, pg, sg, pc, sc, ps, ss, ph, sh)
     return h
 
 
@@ -241,23 +233,23 @@ def distill_loss(logits, teacher, index, temperature=1.0, weight=None, *, grad=T
     and the gradient of the losses' sum by the logits, in their type (None without grad).  weight: a float per row; rows of weight
     0 are left out.  out: a tensor for dlogits (may be logits)."""
     px, sx = _rows("logits", logits)
-    rows, classes = logits.shape
+    rows, classes = shape = logits.shape
     if not isinstance(teacher, torch.Tensor) or teacher.dim() != 2:
         _refuse("teacher is not a 2-D tensor")
+    if teacher.dtype not in DTYPES:
+        _refuse("teacher is of type %s" % (teacher.dtype,))
     top = teacher.size(1)
-    pt, st = _rows("teacher", teacher, logits, shape=(rows, top))
-    pi, si = _rows("index", index, logits, dtypes=_INDEX, shape=(rows, top))
+    pt, st = _rows("teacher", teacher, logits, (teacher.dtype,), (rows, top))
+    pi, si = _rows("index", index, logits, _INDEX, (rows, top))
+    pw = _floats("weight", weight, logits, rows)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     dlogits, pd, sd = None, None, 0
     if grad:
-        dlogits = torch.empty((rows, classes), dtype=logits.dtype, device=logits.device) if out is None else out
-        pd, sd = _rows("out", dlogits, logits, shape=(rows, classes))
-        _same_type("out", dlogits, logits)
+        dlogits = _new(logits) if out is None else out
+        pd, sd = _rows("out", dlogits, logits, shape=shape)
     elif out is not None:
         _refuse("out without grad")
-    with _On(logits) as stream:
-        ws, nb = _workspace("amp_distill_workspace", logits)
-        _check(B.lib().amp_distill_loss(DTYPES[logits.dtype], rows, classes, px, sx, top, DTYPES[teacher.dtype], pt, st, pi, _INDEX[index.dtype],
-                                        si, temperature, _floats("weight", weight, logits, rows), loss.data_ptr(), pd, sd, _ptr(ws), nb,
-                                        stream))
+    ws, nb = _workspace("amp_distill_workspace", logits)
+    _call(logits, "amp_distill_loss", DTYPES[logits.dtype], rows, classes, px, sx, top, DTYPES[teacher.dtype], pt, st, pi, _INDEX[index.dtype],
+          si, temperature, pw, loss.data_ptr(), pd, sd, _ptr(ws), nb)
     return loss, dlogits
