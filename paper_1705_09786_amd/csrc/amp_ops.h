@@ -42,7 +42,7 @@ struct ScanStepArgs {
 };
 
 struct DistillArgs {
-  size_t rows, classes;
+  size_t rows, classes, row0;   // row0: a launch's first row
   const void* logits;
   size_t logits_stride;
   int top, teacher_dtype, index_bytes;

@@ -8,6 +8,7 @@ typedef _Float16 f16;
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef f16 v2h __attribute__((ext_vector_type(2)));
 
