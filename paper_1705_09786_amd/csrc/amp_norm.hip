@@ -207,7 +207,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
   }
   if (!a.dweight && !a.dbias) return;
   // the rows that the workgroup's waves have side by side are joined first, in their order
-  float* out = a.workspace + (size_t)blockIdx.x * 2 * a.cols;
+  float *out_w = a.workspace + (size_t)blockIdx.x * 2 * a.cols, *out_b = out_w + a.cols;
+  if (gridDim.x == 1) out_w = a.dweight, out_b = a.dbias;   // the only part is the sum
   if constexpr (RPW == 1) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -215,8 +216,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
 #pragma unroll
         for (int k = 0; k < N; ++k)
           if (R.counts(j, k)) {
-            out[R.at(j) + k] = dw[j][k];
-            out[a.cols + R.at(j) + k] = db[j][k];
+            if (out_w) out_w[R.at(j) + k] = dw[j][k];
+            if (out_b) out_b[R.at(j) + k] = db[j][k];
           }
   } else {
     constexpr int SPAN = TPR * N;   // columns of a group number
@@ -241,8 +242,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_backward_kernel(No
                 sw += both[0][i][R.lane * N + k];
                 sb += both[1][i][R.lane * N + k];
               }
-              out[R.at(j) + k] = sw;
-              out[a.cols + R.at(j) + k] = sb;
+              if (out_w) out_w[R.at(j) + k] = sw;
+              if (out_b) out_b[R.at(j) + k] = sb;
             }
       }
   }
@@ -430,7 +431,8 @@ hipError_t backward(const Shape& s, const NormArgs* a, hipStream_t stream) {
 }  // namespace
 
 extern "C" size_t amp_norm_workspace_bytes(int dtype, size_t rows, size_t cols) {
-  return ((size_t)shape_of(dtype, rows, cols, true).parts * 2 * cols * sizeof(float) + 15) / 16 * 16;
+  const Shape s = shape_of(dtype, rows, cols, true);
+  return s.tpr && s.parts == 1 ? 0 : ((size_t)s.parts * 2 * cols * sizeof(float) + 15) / 16 * 16;
 }
 
 extern "C" hipError_t amp_norm_forward_launch(int dtype, const NormArgs* a, hipStream_t stream) {
@@ -442,7 +444,7 @@ extern "C" hipError_t amp_norm_backward_launch(int dtype, const NormArgs* a, hip
   const Shape s = shape_of(dtype, a->rows, a->cols, true);
   hipError_t e = hipSuccess;
   if (a->rows) OPS_BY_TYPE(dtype, e = backward<T>(s, a, stream));
-  if (e == hipSuccess && (a->dweight || a->dbias))
+  if (e == hipSuccess && (a->dweight || a->dbias) && !(s.tpr && s.parts == 1))
     e = launch(norm_join_kernel, dim3((unsigned)((2 * a->cols + 31) / 32)), dim3(32 * JOIN), 0, stream, *a, a->rows ? s.parts : 0);
   return e;
 }

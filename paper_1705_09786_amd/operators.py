@@ -73,7 +73,7 @@ def _floats(name, x, like, *shape):
     """A contiguous float32 tensor of that shape, or None: its address."""
     if x is None:
         return None
-    if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.device != like.device:
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.get_device() != like.get_device():
         _refuse("%s is not a contiguous float32 tensor of shape %s on %s" % (name, shape, like.device))
     return x.data_ptr()
 
@@ -110,7 +110,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, stats=False, out=None):
     pw, pb = _floats("weight", weight, x, cols), _floats("bias", bias, x, cols)
     mean = rstd = None
     if stats:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
     _call(x, "amp_layer_norm_forward", DTYPES[x.dtype], rows, cols, px, sx, pw, pb, eps, py, sy, _ptr(mean), _ptr(rstd))
     return (y, mean, rstd) if stats else y
 
@@ -126,7 +127,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, *, out=None):
     if mean is None or rstd is None:
         _refuse("mean and rstd are needed")
     pm, pr, pw = _floats("mean", mean, x, rows), _floats("rstd", rstd, x, rows), _floats("weight", weight, x, cols)
-    dweight, dbias = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+    dweight = torch.empty(cols, dtype=torch.float32, device=x.device)
+    dbias = torch.empty_like(dweight)
     ws, n = _workspace("amp_layer_norm_workspace", x)
     _call(x, "amp_layer_norm_backward", DTYPES[x.dtype], rows, cols, pd, sd, px, sx, pw, pm, pr, po, so, dweight.data_ptr(), dbias.data_ptr(),
           _ptr(ws), n)
