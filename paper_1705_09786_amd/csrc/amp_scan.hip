@@ -7,8 +7,9 @@
 //
 // One pass over the data: a workgroup reads a tile once, publishes its map as one 64-bit word per feature, finds the state that
 // comes in from the words of the tiles in front, and writes its rows.  A word is {P, Q}; once the state behind the tile is known it
-// is replaced by the map that gives it, {cut, state}, so a reader goes back to the nearest cut and applies the maps from there on
-// in the rows' order.  Each state is one fma of the state in front of it whichever word a reader met: results do not depend on timing.
+// is replaced by the map that gives it, {cut, state}, so a reader goes back to the nearest cut.  Four tiles share a second word in
+// the same way, and the chain of the states runs over those.  States are formed from the same maps in the same order whichever word a
+// reader met: results do not depend on timing.
 #include "amp_ops.hip.h"
 #include "amp_common.hip.h"
 
@@ -319,13 +320,15 @@ __device__ __forceinline__ void tile_map(const Maps<L>& m, int c, float& p, floa
 }
 
 // ------------------------------------------------------------------ the hand-over between tiles
-// Workspace: a ticket counter for every CH features, 64 bytes apart, then a word for every tile and slot, then the rows' flags and
-// sequences, the same for all features.  Counters and words are EMPTY before the kernel; no map has those bits (a NaN is published
-// as the one below).  The tiles of CH features are taken by ticket, in the order in which their states follow each other: a workgroup
-// waits only for tiles that running workgroups have taken, so every wait ends whatever else the GPU does.  (Another call writing the
-// same workspace at the same time would break that: a wait is given up after some seconds, and the states become NaN.)
-constexpr int FAR = 16;    // tiles in front that a wait looks at
-constexpr int AHEAD = 8;   // words on their way together
+// Workspace: a ticket counter for every CH features, 64 bytes apart, then a word for every tile and slot and one for every group of
+// tiles and slot, then the rows' flags and sequences, the same for all features.  Counters and words are EMPTY before the kernel; no map has
+// those bits (a NaN is published as the one below).  The tiles of CH features are taken by ticket, in the order in which their states
+// follow each other (the backward pass: from the last on): a workgroup waits only for tiles that running workgroups have taken, so
+// every wait ends whatever else the GPU does.  (Another call writing the same workspace at the same time would break that: a wait
+// is given up after some seconds, and the states become NaN.)
+constexpr int GROUP = 4;   // tiles that share a word
+constexpr int FAR = 16;    // groups in front that a wait looks at
+constexpr int AHEAD = 4;   // words of them on their way together
 constexpr unsigned EMPTY = 0xffffffffu, PUBLISHED_NAN = 0x7fc00000u;
 constexpr long WAIT_TICKS = 500000000;   // of the 100 MHz clock
 
@@ -342,75 +345,104 @@ __device__ __forceinline__ bool word_cut(unsigned long long w) { return (unsigne
 
 struct Hand {
   unsigned* tickets;
-  unsigned long long* words;
+  unsigned long long *words, *groups;
   int* seq;
   unsigned char* flag;
   size_t tiles, slots;   // slots: the features in whole workgroups
   static constexpr int MOST_CH = 128;
   __host__ __device__ static size_t slots_of(size_t hidden) { return (hidden + MOST_CH - 1) / MOST_CH * MOST_CH; }
   // a ticket counter for every 64 slots, words for all slots
-  __host__ __device__ static size_t clear_bytes(size_t tiles, size_t hidden) { return slots_of(hidden) * (1 + tiles * 8); }
+  __host__ __device__ static size_t clear_bytes(size_t tiles, size_t hidden) { return slots_of(hidden) * (1 + (tiles + tiles / GROUP) * 8); }
   __device__ Hand(const ScanArgs& a, size_t tiles_) : tiles(tiles_), slots(slots_of(a.hidden)) {
     tickets = (unsigned*)a.workspace;
     words = (unsigned long long*)((char*)a.workspace + slots);
+    groups = words + tiles * slots;
     seq = (int*)((char*)a.workspace + clear_bytes(tiles, a.hidden));
     flag = (unsigned char*)(seq + tiles * TILE);
   }
-  __device__ unsigned long long load(size_t tile, size_t ch) const {
-    return __hip_atomic_load(words + tile * slots + ch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __device__ unsigned long long load(const unsigned long long* of, size_t i, size_t slot) const {
+    return __hip_atomic_load(of + i * slots + slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  __device__ void store(size_t tile, size_t ch, float p, float q) const {
-    __hip_atomic_store(words + tile * slots + ch, word_of(p, q), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __device__ void store(unsigned long long* of, size_t i, size_t slot, float p, float q) const {
+    __hip_atomic_store(of + i * slots + slot, word_of(p, q), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 };
 
-// One wave, a slot to a lane: publishes the tile's map, finds what comes into the tile (returned), and publishes what goes out of
-// it.  A wait looks at the words of the tile in front, which are mostly what it needs, and at one word of each of FAR tiles: where the
-// states behind the nearest are not known yet, they are formed from the nearest known ones over the maps between.  (Looking at 64
-// tiles costs every wait 48 lines: 1 .. 3 % where tiles are short of nothing; looking at 8 makes long chains slower, 524,288 x 256
-// bf16 870 us for 731.)
-template <bool BACK>
+// One wave, a slot to a lane: publishes the tile's map and returns what comes into the tile: what comes into its group of GROUP tiles,
+// through the maps of the group's tiles in front.  A group's last tile publishes the group's map, and once what comes into the group is
+// known the map that gives what goes out.  A wait for that looks at the word of the group in front, which is mostly what it needs, and
+// at one word of each of FAR groups: where the state behind the nearest is not known yet, it is formed from the nearest known one over
+// the maps between, up to AHEAD words on their way together.
+// A chain of states over single tiles costs 0.17 us a tile, and that is the time of a call with few features, whose tiles all run at
+// once; in groups it is 0.07 (one sequence of 524,288 x 256 bf16: 709 and 285 us; 131,072 x 640: 209 and 141; 65,536 x 2,048: 198 and
+// 185).  The group's words cost 2 to 4 % where no chain is waited for (the backward pass of 65,536 x 2,048: 324 and 332 us).
 __device__ __forceinline__ float hand_over(const Hand& h, size_t order, size_t slot0, float p, float q) {
-  const int lane = threadIdx.x & 63;
-  const size_t slot = slot0 + lane;
-  const auto tile_at = [&](size_t o) { return BACK ? h.tiles - 1 - o : o; };
-  if (order == 0) {
-    h.store(tile_at(0), slot, __uint_as_float(CUT), apply(p, q, 0.f));
-    return 0.f;
-  }
-  h.store(tile_at(order), slot, p, q);
-  const int far = order < FAR ? (int)order : FAR;
+  const int lane = threadIdx.x & 63, r = (int)(order % GROUP);
+  const size_t slot = slot0 + lane, g = order / GROUP, first = order - r;
+  const bool closes = r == GROUP - 1;
+  const int far = g < FAR ? (int)g : FAR;
+  if (!closes) h.store(h.words, order, slot, p, q);
+  float lp = 1.f, lq = 0.f, gp = p, gq = q, x = 0.f;   // the maps of the group's tiles in front, and with this one; what comes into the group
+  bool local = r == 0, known = g == 0;
   const long began = wall_clock64();
   for (;;) {
-    const unsigned long long next = h.load(tile_at(order - 1), slot), s = lane < far ? h.load(tile_at(order - 1 - lane), slot0) : ~0ull;
-    const unsigned long long cuts = __ballot(word_there(s) && word_cut(s)), there = __ballot(word_there(s));
-    int n = cuts ? __ffsll(cuts) : 0;   // tiles to go back to
-    if (n && (~there & ~0ull >> (64 - n))) n = 0;   // (one between is missing)
-    if (__all(word_there(next) && word_cut(next))) n = 1;
-    if (n) {
-      float x = 0.f;
+    unsigned long long w[GROUP - 1], next = 0, s = ~0ull;
+    if (!local)
+#pragma unroll
+      for (int i = 0; i < GROUP - 1; ++i)
+        if (i < r) w[i] = h.load(h.words, first + i, slot);
+    if (!known) {
+      next = h.load(h.groups, g - 1, slot);
+      if (lane < far) s = h.load(h.groups, g - 1 - lane, slot0);
+    }
+    if (!local) {
       bool all = true;
-      for (int at = n; at > 0; at -= AHEAD) {   // from the farthest on, up to AHEAD words on their way together
-        unsigned long long w[AHEAD];
+      lp = 1.f, lq = 0.f;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-          if (at - i > 1) w[i] = h.load(tile_at(order - (at - i)), slot);
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-          if (at - i > 0) {
-            const unsigned long long v = at - i > 1 ? w[i] : next;
-            all = all && word_there(v) && (at - i < n || word_cut(v));
-            x = apply(word_p(v), word_q(v), x);
-          }
-      }
-      if (__all(all)) {
-        // a tile that cuts the states itself has published what goes out already
-        if (!__all(is_cut(p))) h.store(tile_at(order), slot, __uint_as_float(CUT), apply(p, q, x));
-        return x;
+      for (int i = 0; i < GROUP - 1; ++i)
+        if (i < r) {
+          all = all && word_there(w[i]);
+          compose(lp, lq, word_p(w[i]), word_q(w[i]));
+        }
+      local = __all(all);
+      if (local) {
+        gp = lp, gq = lq;
+        compose(gp, gq, p, q);
+        if (closes) h.store(h.groups, g, slot, gp, gq);
       }
     }
+    if (local && __all(is_cut(lp))) return lq;   // a sequence begins in the group's tiles in front
+    if (!known) {
+      const unsigned long long cuts = __ballot(word_there(s) && word_cut(s)), there = __ballot(word_there(s));
+      int n = cuts ? __ffsll(cuts) : 0;   // groups to go back to
+      if (n && (~there & ~0ull >> (64 - n))) n = 0;   // (one between is missing)
+      if (__all(word_there(next) && word_cut(next))) n = 1;
+      if (n) {
+        bool all = true;
+        x = 0.f;
+        for (int at = n; at > 0; at -= AHEAD) {   // from the farthest on, up to AHEAD words on their way together
+          unsigned long long v[AHEAD];
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i)
+            if (at - i > 1) v[i] = h.load(h.groups, g - (at - i), slot);
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i)
+            if (at - i > 0) {
+              const unsigned long long u = at - i > 1 ? v[i] : next;
+              all = all && word_there(u) && (at - i < n || word_cut(u));
+              x = apply(word_p(u), word_q(u), x);
+            }
+        }
+        known = __all(all);
+      }
+    }
+    if (local && known) {
+      // a group that cuts the states itself has published what goes out already
+      if (closes && !__all(is_cut(gp))) h.store(h.groups, g, slot, __uint_as_float(CUT), apply(gp, gq, x));
+      return apply(lp, lq, x);
+    }
     if (wall_clock64() - began > WAIT_TICKS) {
-      h.store(tile_at(order), slot, __uint_as_float(CUT), __uint_as_float(PUBLISHED_NAN));
+      if (closes) h.store(h.groups, g, slot, __uint_as_float(CUT), __uint_as_float(PUBLISHED_NAN));
       return __uint_as_float(PUBLISHED_NAN);
     }
     __builtin_amdgcn_s_sleep(2);
@@ -548,7 +580,7 @@ __global__ __launch_bounds__(TPB, 4) void scan_forward_kernel(ScanArgs a, size_t
     if (tiles > 1) {
       float tp, tq;
       tile_map<L, false>(m, threadIdx.x, tp, tq);
-      x = hand_over<false>(hand, order, c0, tp, tq);
+      x = hand_over(hand, order, c0, tp, tq);
     }
     into_parts<L, false>(m, threadIdx.x, x, into);
   }
@@ -658,7 +690,7 @@ __global__ __launch_bounds__(TPB, 2) void scan_backward_kernel(ScanArgs a, size_
     if (tiles > 1) {
       float tp, tq;
       tile_map<L, true>(back, threadIdx.x, tp, tq);
-      in = hand_over<true>(hand, order, c0, tp, tq);
+      in = hand_over(hand, order, c0, tp, tq);
     }
     into_parts<L, true>(back, threadIdx.x, in, into);
   } else if (threadIdx.x < 2 * L::CH) {   // beside it
@@ -725,13 +757,13 @@ size_t bytes_of(size_t tiles, size_t hidden) {
 }
 
 template <class L, bool BACK>
-hipError_t run(void (*kernel)(ScanArgs, size_t), const ScanArgs* a, hipStream_t stream) {
-  const size_t tiles = tiles_of(a->rows), blocks = (a->hidden + L::CH - 1) / L::CH;
+hipError_t run(void (*kernel)(ScanArgs, size_t), const ScanArgs& a, hipStream_t stream) {
+  const size_t tiles = tiles_of(a.rows), blocks = (a.hidden + L::CH - 1) / L::CH;
   if (tiles > 1) {
-    const hipError_t e = launch(scan_plan_kernel<BACK>, dim3((unsigned)(tiles < 1024 ? tiles : 1024)), dim3(TPB), 0, stream, *a, tiles);
+    const hipError_t e = launch(scan_plan_kernel<BACK>, dim3((unsigned)(tiles < 1024 ? tiles : 1024)), dim3(TPB), 0, stream, a, tiles);
     if (e != hipSuccess) return e;
   }
-  return launch(kernel, dim3((unsigned)(blocks * tiles)), dim3(TPB), 0, stream, *a, tiles);
+  return launch(kernel, dim3((unsigned)(blocks * tiles)), dim3(TPB), 0, stream, a, tiles);
 }
 
 }  // namespace
@@ -743,12 +775,12 @@ namespace {
 template <class T, bool NARROW>
 hipError_t forward(int tanh, const ScanArgs* a, hipStream_t stream) {
   typedef Lay<T, NARROW> L;
-  return run<L, false>(tanh ? scan_forward_kernel<L, true> : scan_forward_kernel<L, false>, a, stream);
+  return run<L, false>(tanh ? scan_forward_kernel<L, true> : scan_forward_kernel<L, false>, *a, stream);
 }
 template <class T, bool NARROW>
 hipError_t backward(int tanh, const ScanArgs* a, hipStream_t stream) {
   typedef Lay<T, NARROW> L;
-  return run<L, true>(tanh ? scan_backward_kernel<L, true> : scan_backward_kernel<L, false>, a, stream);
+  return run<L, true>(tanh ? scan_backward_kernel<L, true> : scan_backward_kernel<L, false>, *a, stream);
 }
 
 }  // namespace

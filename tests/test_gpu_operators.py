@@ -167,6 +167,7 @@ SCANS = [  # rows, hidden, sequences
     (400, 40, packed([2, 5, 1, 0, 4] * 30)),
     (64, 16, packed([0, 0, 0])),                                                              # rows, and none in a sequence
     (2600, 9, packed([1] * 700 + [0] * 600 + [900, 1000])),                                   # more sequences than a tile has threads
+    (1400, 1090, packed([700, 1, 0, 699])), (1700, 12, packed([1650, 50])),                   # wide and narrow: tiles alone and in groups
 ]
 
 
