@@ -535,12 +535,14 @@ typedef struct amp_sequences {
 
 /* Gated linear recurrence: per feature
  *   z_t = sigmoid(gate_t), v_t = act(cand_t), h_t = (1 - z_t) h_{t-1} + z_t v_t
- * along every sequence (fewer than 2^30 rows, hidden and strides below 2^22), h before its first row = h0[s] (n x hidden floats;
+ * along every sequence, h before its first row = h0[s] (n x hidden floats;
  * NULL = zeros): the GRU's update of its state, the gates formed from the
- * inputs alone.  activation: AMP_ACT_NONE or AMP_ACT_TANH.  h (may be NULL)
+ * inputs alone.  Fewer than 2^30 rows, hidden and strides below 2^22, up to
+ * 2^36 elements.  activation: AMP_ACT_NONE or AMP_ACT_TANH.  h (may be NULL)
  * gets every row's state in the inputs' type; last (n x hidden floats, may be
- * NULL) the state behind every sequence's last row, h0 for an empty one.  carry (may be NULL): the states that the backward pass
- * starts from, amp_gated_scan_carry rows x hidden floats. */
+ * NULL) the state behind every sequence's last row, h0 for an empty one.
+ * carry (may be NULL): the states that the backward pass starts from,
+ * amp_gated_scan_carry rows x hidden floats. */
 int amp_gated_scan_carry(int dtype, size_t rows, size_t hidden, size_t *carry_rows);
 int amp_gated_scan_workspace(int dtype, size_t rows, size_t hidden, size_t *bytes);   /* of either direction */
 int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden, const void *gate, size_t gate_stride, const void *cand,

@@ -105,6 +105,8 @@ int check_scan_size(const char* what, int dtype, size_t rows, size_t hidden) {
   CHECK(check_size(what, dtype, rows, hidden, "hidden"));
   if (rows >= MAX_ROWS / 2) return fail(AMP_EINVAL, "%s: %zu rows, fewer than 2^30 are taken", what, rows);
   if (hidden >= (size_t)1 << 22) return fail(AMP_EINVAL, "%s: hidden = %zu, 1 .. 2^22 - 1 are taken", what, hidden);
+  // a launch has fewer than 2^24 workgroups of 256 threads, each of them 128 rows by 64 features
+  if (rows > ((size_t)1 << 36) / hidden) return fail(AMP_EINVAL, "%s: %zu rows of %zu, up to 2^36 elements are taken", what, rows, hidden);
   return AMP_OK;
 }
 

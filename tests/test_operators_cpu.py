@@ -126,6 +126,9 @@ def test_scan_workspace_is_checked():
         refused(scan_forward(rows=100000, h=P + 16 * MB, cand=P + 8 * MB, ws=None), "workspace")
         refused(scan_forward(rows=100000, h=P + 16 * MB, cand=P + 8 * MB, ws=P + 32 * MB + 8), "workspace")
     assert B.lib().amp_gated_scan_carry(B.F32, 0, 8, ct.byref(n)) == B.AMP_OK
+    assert B.lib().amp_gated_scan_workspace(B.F32, 1 << 22, 1 << 14, ct.byref(n)) == B.AMP_OK
+    refused(B.lib().amp_gated_scan_workspace(B.F32, (1 << 22) + 1, 1 << 14, ct.byref(n)), "elements")
+    refused(scan_forward(rows=(1 << 24) + 1, hidden=1 << 12, gs=0, cs=0, h=None), "elements")
     refused(B.lib().amp_gated_scan_carry(B.F32, 5, 8, None), "carry_rows")
     refused(B.lib().amp_gated_scan_workspace(5, 5, 8, ct.byref(n)), "dtype")
 
