@@ -495,6 +495,79 @@ def test_wrappers_refuse():
             pytest.fail("call %d was taken" % k)
 
 
+# ------------------------------------------------------------------ long and many
+def test_offsets_past_32_bits():
+    """Rows so far apart that the last ones begin behind 2^32 elements: the bits of the same rows next to each other."""
+    rows, cols, step = 1100, 40, 4000000
+    big = torch.empty(rows * step, dtype=torch.bfloat16, device="cuda")
+    at = [big.as_strided((rows, cols), (step, 1), 64 * k) for k in range(5)]
+    x = [dev(rand(rows, cols, seed=200 + k, dtype=torch.bfloat16)) for k in range(3)]
+    for a, v in zip(at, x):
+        a.copy_(v)
+    w = dev(rand(cols, seed=203, shift=1.0))
+    y, mean, rstd = ops.layer_norm(x[0], w, stats=True)
+    assert same_bits(ops.layer_norm(at[0], w, out=at[3]), y)
+    want = ops.layer_norm_backward(x[1], x[0], w, mean, rstd)
+    got = ops.layer_norm_backward(at[1], at[0], w, mean, rstd, out=at[3])
+    assert all(same_bits(p, q) for p, q in zip(got, want))
+    seq = dev(torch.tensor([0, 300, 301, 1097]))
+    want = ops.gated_scan(x[0], x[1], seq, activation="tanh", last=True, carry=True, out=dev(torch.zeros_like(x[0])))
+    at[3].zero_()
+    got = ops.gated_scan(at[0], at[1], seq, activation="tanh", last=True, carry=True, out=at[3])
+    assert all(same_bits(p, q) for p, q in zip(got, want))
+    carry = want[2]
+    want = ops.gated_scan_backward(x[2], x[0], x[1], carry, seq, activation="tanh", out=(dev(torch.zeros_like(x[0])), dev(torch.zeros_like(x[0]))))
+    at[3].zero_(), at[4].zero_()
+    got = ops.gated_scan_backward(at[2], at[0], at[1], carry, seq, activation="tanh", out=(at[3], at[4]))
+    assert all(same_bits(p, q) for p, q in zip(got, want))
+    state = dev(rand(rows, cols, seed=204))
+    other = state.clone()
+    assert same_bits(ops.gated_scan_step(at[0], at[1], other, out=at[3]), ops.gated_scan_step(x[0], x[1], state)) and same_bits(other, state)
+    index = dev(torch.arange(rows)[:, None] % cols + torch.zeros(1, 3, dtype=torch.long))
+    want = ops.distill_loss(x[0], x[1][:, :3], index, 2.0)
+    got = ops.distill_loss(at[0], at[1][:, :3], index, 2.0, out=at[3])
+    assert all(same_bits(p, q) for p, q in zip(got, want))
+
+
+def test_more_rows_than_workgroups():
+    """Every row of a call with millions of them is that of a call with a few."""
+    n, c = (1 << 21) + 1500, 5
+    x, index = dev(rand(n, c, seed=210)), dev(torch.arange(n)[:, None] % c)
+    w, dy = dev(rand(c, seed=211)), dev(rand(n, c, seed=212))
+    loss, grad = ops.distill_loss(x, dy[:, :1], index)
+    y, mean, rstd = ops.layer_norm(x, w, stats=True)
+    dx = ops.layer_norm_backward(dy, x, w, mean, rstd)[0]
+    state = x.clone()
+    h = ops.gated_scan_step(dy, x, state)
+    for s in (slice(0, 700), slice(n - 1600, n)):
+        few = [t[s].contiguous() for t in (x, dy, index, mean, rstd)]
+        assert all(same_bits(p[s], q) for p, q in zip((loss, grad), ops.distill_loss(few[0], few[1][:, :1], few[2])))
+        assert same_bits(y[s], ops.layer_norm(few[0], w)) and same_bits(dx[s], ops.layer_norm_backward(few[1], few[0], w, *few[3:])[0])
+        assert same_bits(h[s], ops.gated_scan_step(few[1], few[0], few[0].clone())) and same_bits(state[s], h[s])
+
+
+@pytest.mark.parametrize("rows", [1, 128, 1000])
+def test_scan_more_sequences_than_rows(rows):
+    """Thousands of empty sequences before, between and behind the others hand their states through, in both directions."""
+    n, hidden = 20000, 70
+    begin = torch.cat([torch.zeros(n // 2, dtype=torch.long), torch.full((n - n // 2,), rows)])
+    end = begin.clone()
+    end[n // 2 - 1] = rows   # the one with rows
+    h0, gate, cand, dh = (rand(n, hidden, seed=220), *(rand(rows, hidden, seed=221 + k) for k in range(3)))
+    dlast = rand(n, hidden, seed=224)
+    seq = (dev(begin), dev(end))
+    h, last, carry = ops.gated_scan(*dev(gate, cand), seq, h0=dev(h0), last=True, carry=True)
+    k = n // 2 - 1
+    alone = ops.gated_scan(*dev(gate, cand), h0=dev(h0[k:k + 1]), last=True, carry=True)
+    assert same_bits(h, alone[0]) and same_bits(last[k], alone[1][0])
+    empty = torch.arange(n) != k
+    assert same_bits(last.cpu()[empty], h0[empty])
+    got = ops.gated_scan_backward(*dev(dh, gate, cand), carry, seq, h0=dev(h0), dlast=dev(dlast))
+    want = ops.gated_scan_backward(*dev(dh, gate, cand), alone[2], h0=dev(h0[k:k + 1]), dlast=dev(dlast[k:k + 1]))
+    assert same_bits(got[0], want[0]) and same_bits(got[1], want[1]) and same_bits(got[2][k], want[2][0])
+    assert same_bits(got[2].cpu()[empty], dlast[empty])
+
+
 # ------------------------------------------------------------------ streams and graphs
 def everything(s):
     """One pass through every operator: norm, recurrence, logits, loss, and all the way back."""

@@ -44,7 +44,7 @@ def test_norm_forward_refusals():
     assert norm_forward(rows=0) == B.AMP_OK   # nothing to do, nothing launched
 
 
-def norm_backward(dtype=B.F32, rows=4, cols=8, dy=P, dys=8, x=P + MB, xs=8, w=None, mean=P + 2 * MB, rstd=P + 3 * MB, dx=P + 4 * MB, dxs=8,
+def norm_backward(dtype=B.F32, rows=400, cols=8, dy=P, dys=8, x=P + MB, xs=8, w=None, mean=P + 2 * MB, rstd=P + 3 * MB, dx=P + 4 * MB, dxs=8,
                   dw=P + 5 * MB, db=P + 6 * MB, ws=P + 7 * MB, n=16 * MB):
     return B.lib().amp_layer_norm_backward(dtype, rows, cols, dy, dys, x, xs, w, mean, rstd, dx, dxs, dw, db, ws, n, None)
 
@@ -63,7 +63,8 @@ def test_norm_backward_refusals():
     refused(norm_backward(ws=P + 5 * MB), "dweight overlaps workspace")
     assert norm_backward(dx=None, dw=None, db=None, ws=None, n=0) == B.AMP_OK
     n = ct.c_size_t()
-    assert B.lib().amp_layer_norm_workspace(B.F32, 4, 8, ct.byref(n)) == B.AMP_OK and n.value > 0
+    assert B.lib().amp_layer_norm_workspace(B.F32, 400, 8, ct.byref(n)) == B.AMP_OK and n.value > 0
+    assert B.lib().amp_layer_norm_workspace(B.F32, 4, 8, ct.byref(n)) == B.AMP_OK and n.value == 0   # one workgroup has all rows
     refused(B.lib().amp_layer_norm_workspace(B.F32, 4, 8, None), "bytes")
 
 
