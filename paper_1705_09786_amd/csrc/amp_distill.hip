@@ -2,7 +2,7 @@
 //
 // Bound by HBM: a workgroup keeps a row of logits in its registers from the sum of the exponentials to the gradient, so that each
 // logit is read once and its gradient written once, at the rate of a copy for rows that leave room for several workgroups on a compute
-// unit (8,192 x 32,000 bf16: 210 us, 5.0 TB/s).  A workgroup has one row: its registers are free for the next one's loads as soon as
+// unit (8,192 x 32,000 bf16: 203 us, 5.2 TB/s).  A workgroup has one row: its registers are free for the next one's loads as soon as
 // its stores are on their way (workgroups that stay and fetch the next row while they write one took 330 us there, waiting for their
 // own stores in front of the loads behind them).
 #include "amp_ops.hip.h"

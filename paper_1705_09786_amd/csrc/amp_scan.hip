@@ -10,6 +10,10 @@
 // is replaced by the map that gives it, {cut, state}, so a reader goes back to the nearest cut.  Four tiles share a second word in
 // the same way, and the chain of the states runs over those.  States are formed from the same maps in the same order whichever word a
 // reader met: results do not depend on timing.
+//
+// What bounds it: HBM where rows are long, 805 MB at 4.4 TB/s for 65,536 x 2,048 bf16 forward (184 us; a large copy runs at 5.2 TB/s),
+// 1.06 GB at 3.9 TB/s for 41,000 x 2,560 bf16 backward (275 us), whose five arrays of a tile leave room for two workgroups on a
+// compute unit, where the forward pass has four.  Where features are few, the chain of the states (hand_over).
 #include "amp_ops.hip.h"
 #include "amp_common.hip.h"
 
