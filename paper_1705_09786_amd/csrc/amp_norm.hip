@@ -354,7 +354,13 @@ __global__ __launch_bounds__(32 * JOIN) void norm_join_kernel(NormArgs a, int pa
   const size_t c = (size_t)blockIdx.x * 32 + lane, cols2 = 2 * a.cols;
   float s = 0.f;
   if (c < cols2)
-    for (int p = share; p < parts; p += JOIN) s += a.workspace[(size_t)p * cols2 + c];
+    for (int p = share; p < parts; p += 8 * JOIN) {
+      float v[8];   // on their way together
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p + i * JOIN < parts ? a.workspace[(size_t)(p + i * JOIN) * cols2 + c] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
   sum[share][lane] = s;
   __syncthreads();
   if (share == 0 && c < cols2) {
