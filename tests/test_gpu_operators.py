@@ -114,6 +114,21 @@ def test_norm_in_place_and_repeated_rows():
         assert same_bits(g, want)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(700, 37), (700, 151), (700, 1021), (30, 2049), (30, 11111), (5, 40001), (3, 70003)])
+def test_norm_in_place_at_odd_sizes(dtype, rows, cols):
+    """Rows whose last group reaches back over elements that another thread writes."""
+    x, dy, w = dev(rand(rows, cols, seed=15, dtype=dtype), rand(rows, cols, seed=16, dtype=dtype), rand(cols, seed=17, shift=1.0))
+    y, mean, rstd = ops.layer_norm(x, w, stats=True)
+    z = x.clone()
+    assert same_bits(ops.layer_norm(z, w, out=z), y)
+    want = ops.layer_norm_backward(dy, x, w, mean, rstd)
+    for place in (0, 1):
+        args = [dy.clone(), x.clone()]
+        got = ops.layer_norm_backward(*args, w, mean, rstd, out=args[place])
+        assert all(same_bits(p, q) for p, q in zip(got, want))
+
+
 def test_norm_without_rows_and_plain_weights():
     x = torch.empty(0, 40, device="cuda")
     y, mean, rstd = ops.layer_norm(x, stats=True)
