@@ -37,10 +37,10 @@ enum { FIRST = 1, LAST = 2, VALID = 4 };
 
 __device__ __forceinline__ bool is_cut(float p) { return __float_as_uint(p) == CUT; }
 __device__ __forceinline__ float apply(float p, float q, float h) { return is_cut(p) ? q : fmaf(p, h, q); }
-// (p, q) then becomes the map of (p, q) followed by (p2, q2).
+// (p, q) then becomes the map of (p, q) followed by (p2, q2).  A cut stays one whatever follows it: p * p2 would not where p2 is no number.
 __device__ __forceinline__ void compose(float& p, float& q, float p2, float q2) {
   q = apply(p2, q2, q);
-  p = is_cut(p2) ? p2 : p * p2;
+  p = is_cut(p) || is_cut(p2) ? __uint_as_float(CUT) : p * p2;
 }
 
 // z = 1 / (1 + e^-g) and keep = 1 - z, both exact to the last bits however near to 0 they are; 0 and 1 at infinite g.
@@ -236,39 +236,49 @@ __device__ __forceinline__ void take_in(const float* states, int flag, const Sca
   }
 }
 
-// The map of a thread's rows, from the first on.  A cut stays one by itself: -0 times a keep is -0.
+// The map of a thread's rows, from the first on.  With a cut among them it is a cut in every feature, whatever their gates hold.
 template <bool PLAIN, class L>
 __device__ __forceinline__ void map_forward(const Flags<L>& f, const float (&keep)[L::LS][L::V], const float (&zv)[L::LS][L::V], float (&p)[L::V],
                                             float (&q)[L::V]) {
+  bool cuts = false;
 #pragma unroll
   for (int k = 0; k < L::V; ++k) p[k] = 1.f, q[k] = 0.f;
 #pragma unroll
   for (int i = 0; i < L::LS; ++i) {
     const bool cut = !PLAIN && (f.of(i) & (FIRST | VALID)) != VALID, none = !PLAIN && !(f.of(i) & VALID);
+    cuts = cuts || cut;
 #pragma unroll
     for (int k = 0; k < L::V; ++k) {
-      const float pk = p[k] * keep[i][k], qk = fmaf(keep[i][k], q[k], zv[i][k]);
-      p[k] = cut ? __uint_as_float(CUT) : pk;
+      const float qk = fmaf(keep[i][k], q[k], zv[i][k]);
+      p[k] *= keep[i][k];
       q[k] = cut ? (none ? 0.f : zv[i][k]) : qk;
     }
   }
+  if (!PLAIN)
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) p[k] = cuts ? __uint_as_float(CUT) : p[k];
 }
 
 // The map of X over a thread's rows, from the last on.
 template <bool PLAIN, class L>
 __device__ __forceinline__ void map_back(const Flags<L>& f, const float (&keep)[L::LS][L::V], const float (&d)[L::LS][L::V], float (&p)[L::V],
                                          float (&q)[L::V]) {
+  bool cuts = false;
 #pragma unroll
   for (int k = 0; k < L::V; ++k) p[k] = 1.f, q[k] = 0.f;
 #pragma unroll
   for (int i = L::LS - 1; i >= 0; --i) {
     const bool cut = !PLAIN && (f.of(i) & (FIRST | VALID)) != VALID;
+    cuts = cuts || cut;
 #pragma unroll
     for (int k = 0; k < L::V; ++k) {
-      p[k] = cut ? __uint_as_float(CUT) : p[k] * keep[i][k];
+      p[k] *= keep[i][k];
       q[k] = cut ? 0.f : keep[i][k] * (q[k] + d[i][k]);
     }
   }
+  if (!PLAIN)
+#pragma unroll
+    for (int k = 0; k < L::V; ++k) p[k] = cuts ? __uint_as_float(CUT) : p[k];
 }
 
 // Per feature, the map of every thread's rows in front of its own (BACK: behind) inside the tile, and the tile's: through LDS, a
@@ -415,7 +425,8 @@ __device__ __forceinline__ float hand_over(const Hand& h, size_t order, size_t s
         if (closes) h.store(h.groups, g, slot, gp, gq);
       }
     }
-    if (local && __all(is_cut(lp))) return lq;   // a sequence begins in the group's tiles in front
+    // a sequence begins in the group's tiles in front (gp is a cut in every lane with lp: what goes out of the group is published)
+    if (local && __all(is_cut(lp))) return lq;
     if (!known) {
       const unsigned long long cuts = __ballot(word_there(s) && word_cut(s)), there = __ballot(word_there(s));
       int n = cuts ? __ffsll(cuts) : 0;   // groups to go back to

@@ -347,6 +347,35 @@ def test_scan_keeps_other_sequences_apart():
     assert got[0][430 - 1].isnan().all()   # and inside a sequence a NaN stays one
 
 
+@pytest.mark.parametrize("lens", [[1536], [300, 1236], [64] * 24])
+@pytest.mark.parametrize("feature", [5, 64, 129])
+def test_scan_keeps_other_features_apart(feature, lens):
+    """A gate that is no number, in every tile of three groups of them in turn: the other features keep their bits, its own the states in
+    front of it and those of other sequences."""
+    rows, hidden = 1536, 130
+    o = packed(lens)
+    seq = torch.tensor(o).cuda()
+    gate, cand, h0, dh, dlast = dev(*scan_inputs(rows, hidden, len(lens), torch.float32, seed=31))
+
+    def run(gate):
+        h, last, carry = ops.gated_scan(gate, cand, seq, h0=h0, last=True, carry=True)
+        return (h, last) + ops.gated_scan_backward(dh, gate, cand, carry, seq, h0=h0, dlast=dlast)
+    want = run(gate)
+    rest = torch.arange(hidden) != feature
+    for r in range(7, rows, 128):
+        bad = gate.clone()
+        bad[r, feature] = NAN
+        got = run(bad)
+        assert all(same_bits(p[:, rest], q[:, rest]) for p, q in zip(got, want)), r
+        s = next(k for k in range(len(lens)) if o[k] <= r < o[k + 1])
+        hit = torch.zeros(rows, dtype=torch.bool)
+        hit[r:o[s + 1]] = True
+        assert got[0][hit, feature].isnan().all() and same_bits(got[0][~hit, feature], want[0][~hit, feature]), r
+        other = torch.arange(len(lens)) != s
+        assert got[1][s, feature].isnan() and got[4][s, feature].isnan(), r
+        assert same_bits(got[1][other, feature], want[1][other, feature]) and same_bits(got[4][other, feature], want[4][other, feature]), r
+
+
 def test_scan_bounds_outside_the_rows():
     """Bounds in front of the first row and behind the last are the nearest row's; descending ones touch nothing outside the arrays."""
     rows, hidden = 300, 33
