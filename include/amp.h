@@ -524,13 +524,14 @@ int amp_layer_norm_backward(int dtype, size_t rows, size_t cols, const void *dy,
  * index_bytes (4 or 8) bytes, ascending and without overlap; end may be
  * begin + 1 of one array of n + 1 offsets.  Lengths of 0 are allowed, and so
  * are rows that belong to no sequence (padding, rows behind the last one):
- * their outputs are left as they were.  Bounds outside the rows are taken for
- * the nearest row, and outputs of sequences that overlap or descend are
- * unspecified.  begin = end = NULL: one sequence (n = 1) of all rows. */
+ * their outputs (h, dgate, dcand) are left as they were, or set to zero with
+ * zero_others = 1.  Bounds outside the rows are taken for the nearest row, and
+ * outputs of sequences that overlap or descend are unspecified.  begin = end = NULL: one sequence (n = 1) of all rows. */
 typedef struct amp_sequences {
   size_t n;
   const void *begin, *end;
   int32_t index_bytes;
+  int32_t zero_others;
 } amp_sequences;
 
 /* Gated linear recurrence: per feature

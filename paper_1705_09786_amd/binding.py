@@ -67,7 +67,8 @@ class EvalResult(ct.Structure):
 
 
 class Sequences(ct.Structure):
-    _fields_ = [("n", ct.c_size_t), ("begin", ct.c_void_p), ("end", ct.c_void_p), ("index_bytes", ct.c_int32)]
+    _fields_ = [("n", ct.c_size_t), ("begin", ct.c_void_p), ("end", ct.c_void_p), ("index_bytes", ct.c_int32),
+                ("zero_others", ct.c_int32)]
 
 
 _ctxp = ct.c_void_p

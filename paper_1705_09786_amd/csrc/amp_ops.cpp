@@ -121,6 +121,7 @@ int check_scan(const char* what, int dtype, int activation, size_t rows, size_t 
     return fail(AMP_EINVAL, "%s: activation %d, AMP_ACT_NONE and AMP_ACT_TANH are taken", what, activation);
   if (!q) return fail(AMP_EINVAL, "%s: sequences is NULL", what);
   if (q->n >= MAX_ROWS) return fail(AMP_EINVAL, "%s: %zu sequences, fewer than 2^31 are taken", what, q->n);
+  if (q->zero_others != 0 && q->zero_others != 1) return fail(AMP_EINVAL, "%s: zero_others %d, 0 and 1 are taken", what, q->zero_others);
   if (!q->begin != !q->end) return fail(AMP_EINVAL, "%s: one of begin and end is NULL", what);
   if (!q->begin) {
     if (q->n > 1) return fail(AMP_EINVAL, "%s: %zu sequences without begin and end", what, q->n);
@@ -220,7 +221,7 @@ int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden
                            float* carry, void* workspace, size_t workspace_bytes, void* hip_stream) {
   const char* what = "gated_scan_forward";
   CHECK(check_scan(what, dtype, activation, rows, hidden, q));
-  if (q->n == 0 || (!h && !last && !carry)) return AMP_OK;
+  if ((q->n == 0 && !q->zero_others) || (!h && !last && !carry)) return AMP_OK;
   if (rows) {
     REQUIRE(gate);
     REQUIRE(cand);
@@ -241,6 +242,7 @@ int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden
   ScanArgs a = {};
   a.rows = rows, a.hidden = hidden, a.gate = gate, a.gate_stride = gate_stride, a.cand = cand, a.cand_stride = cand_stride;
   a.n_seq = n, a.begin = q->begin, a.end = q->end, a.index_bytes = q->index_bytes, a.h0 = h0, a.h = h, a.h_stride = h_stride;
+  a.zero_others = q->zero_others;
   a.last = last, a.carry = carry, a.workspace = workspace;
   return launched(what, amp_scan_forward_launch(dtype, activation == AMP_ACT_TANH, &a, (hipStream_t)hip_stream));
 }
@@ -251,7 +253,7 @@ int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidde
                             float* dh0, void* workspace, size_t workspace_bytes, void* hip_stream) {
   const char* what = "gated_scan_backward";
   CHECK(check_scan(what, dtype, activation, rows, hidden, q));
-  if (q->n == 0) return AMP_OK;
+  if (q->n == 0 && !q->zero_others) return AMP_OK;
   if (rows) {
     REQUIRE(dh);
     REQUIRE(gate);
@@ -279,7 +281,7 @@ int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidde
   ScanArgs a = {};
   a.rows = rows, a.hidden = hidden, a.dh = dh, a.dh_stride = dh_stride, a.dlast = dlast, a.gate = gate, a.gate_stride = gate_stride;
   a.cand = cand, a.cand_stride = cand_stride, a.n_seq = n, a.begin = q->begin, a.end = q->end, a.index_bytes = q->index_bytes;
-  a.h0 = h0, a.carry_in = carry, a.dgate = dgate, a.dgate_stride = dgate_stride, a.dcand = dcand, a.dcand_stride = dcand_stride;
+  a.zero_others = q->zero_others, a.h0 = h0, a.carry_in = carry, a.dgate = dgate, a.dgate_stride = dgate_stride, a.dcand = dcand, a.dcand_stride = dcand_stride;
   a.dh0 = dh0, a.workspace = workspace;
   return launched(what, amp_scan_backward_launch(dtype, activation == AMP_ACT_TANH, &a, (hipStream_t)hip_stream));
 }
@@ -287,7 +289,7 @@ int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidde
 int amp_gated_scan_step(int dtype, int activation, size_t rows, size_t hidden, const void* gate, size_t gate_stride, const void* cand,
                         size_t cand_stride, float* state, size_t state_stride, void* h, size_t h_stride, void* hip_stream) {
   const char* what = "gated_scan_step";
-  const amp_sequences one = {1, nullptr, nullptr, 0};
+  const amp_sequences one = {1, nullptr, nullptr, 0, 0};
   CHECK(check_scan(what, dtype, activation, rows, hidden, &one));
   if (rows == 0) return AMP_OK;
   REQUIRE(gate);

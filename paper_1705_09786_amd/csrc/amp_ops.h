@@ -23,7 +23,7 @@ struct ScanArgs {
   size_t gate_stride, cand_stride, dh_stride;
   size_t n_seq;
   const void *begin, *end;
-  int index_bytes;
+  int index_bytes, zero_others;
   const float *h0, *dlast, *carry_in;
   void *h, *dgate, *dcand;
   size_t h_stride, dgate_stride, dcand_stride;

@@ -33,7 +33,7 @@ struct Lay {
 };
 
 constexpr unsigned CUT = 0x80000000u;
-enum { FIRST = 1, LAST = 2, VALID = 4 };
+enum { FIRST = 1, LAST = 2, VALID = 4, ZERO = 8 };   // ZERO: a row of no sequence whose outputs are to be zeros
 
 __device__ __forceinline__ bool is_cut(float p) { return __float_as_uint(p) == CUT; }
 __device__ __forceinline__ float apply(float p, float q, float h) { return is_cut(p) ? q : fmaf(p, h, q); }
@@ -59,7 +59,7 @@ __device__ __forceinline__ long bound_at(const void* p, int bytes, size_t s, lon
 
 struct TileRows {
   int seq[TILE];                         // the sequence of a row, where it has one
-  alignas(16) unsigned char flag[TILE];  // FIRST, LAST, VALID
+  alignas(16) unsigned char flag[TILE];  // FIRST, LAST, VALID, ZERO
   int part[TPB / 64];
 };
 
@@ -68,13 +68,14 @@ struct TileRows {
 __device__ __forceinline__ void tile_rows(const ScanArgs& a, long t0, TileRows& t, size_t& s0, size_t& s1) {
   const long rows = (long)a.rows, t1 = t0 + TILE;
   const int i = threadIdx.x;
-  if (!a.begin) {
+  const int none = a.zero_others ? ZERO : 0;
+  if (!a.begin) {   // one sequence, or none at all
     if (i < TILE) {
       t.seq[i] = 0;
-      t.flag[i] = t0 + i < rows ? VALID | (t0 + i == 0 ? FIRST : 0) | (t0 + i == rows - 1 ? LAST : 0) : 0;
+      t.flag[i] = t0 + i >= rows ? 0 : !a.n_seq ? none : VALID | (t0 + i == 0 ? FIRST : 0) | (t0 + i == rows - 1 ? LAST : 0);
     }
     s0 = 0;
-    s1 = t0 == 0;
+    s1 = t0 == 0 && a.n_seq;
     __syncthreads();
     return;
   }
@@ -116,7 +117,7 @@ __device__ __forceinline__ void tile_rows(const ScanArgs& a, long t0, TileRows& 
   for (int w = 0; w < TILE / 64; ++w)
     if (w < (i >> 6) && t.part[w] > s) s = t.part[w];
   if (i < TILE) {
-    int f = 0;
+    int f = t0 + i < rows ? none : 0;
     if (s >= 0 && t0 + i < rows) {
       const long b = bound_at(a.begin, a.index_bytes, s, 0, rows), e = bound_at(a.end, a.index_bytes, s, b, rows), r = t0 + i;
       if (r >= b && r < e) f = VALID | (r == b ? FIRST : 0) | (r == e - 1 ? LAST : 0);
@@ -551,7 +552,11 @@ __device__ __forceinline__ void write_forward(const ScanArgs& a, const TileRows&
       const float next = fmaf(keep[i][k], h[k], zv[i][k]);
       h[k] = first ? zv[i][k] : next;
     }
-    if (a.h && (PLAIN || (f.of(i) & VALID))) store_vec(out.row(i), pack<T>(h), L::NARROW ? at.n : L::V);
+    if (a.h && (PLAIN || (f.of(i) & (VALID | ZERO)))) {
+      Vec<T, L::V> o = pack<T>(h);
+      if (!PLAIN && (f.of(i) & ZERO)) o = {};
+      store_vec(out.row(i), o, L::NARROW ? at.n : L::V);
+    }
     if (!PLAIN && (f.of(i) & LAST) && a.last) store_state<L>(a.last, t.seq[at.grp * L::LS + i], a, at, h);
   }
 }
@@ -641,9 +646,11 @@ __device__ __forceinline__ void write_back(const ScanArgs& a, const TileRows& t,
       og[k] = zG * keep[i][k] * (v[i][k] - h[i][k]);
       oc[k] = TANH ? zG * fmaf(-v[i][k], v[i][k], 1.f) : zG;
     }
-    if (PLAIN || (f.of(i) & VALID)) {
-      store_vec(out_g.row(i), pack<T>(og), L::NARROW ? at.n : L::V);
-      store_vec(out_c.row(i), pack<T>(oc), L::NARROW ? at.n : L::V);
+    if (PLAIN || (f.of(i) & (VALID | ZERO))) {
+      Vec<T, L::V> vg = pack<T>(og), vc = pack<T>(oc);
+      if (!PLAIN && (f.of(i) & ZERO)) vg = vc = {};
+      store_vec(out_g.row(i), vg, L::NARROW ? at.n : L::V);
+      store_vec(out_c.row(i), vc, L::NARROW ? at.n : L::V);
     }
     if (!PLAIN && (f.of(i) & FIRST) && a.dh0) store_state<L>(a.dh0, t.seq[at.grp * L::LS + i], a, at, x);
     if (!PLAIN)

@@ -136,10 +136,11 @@ def layer_norm_backward(dy, x, weight, mean, rstd, *, out=None):
 
 
 # ------------------------------------------------------------------ gated linear recurrence
-def _sequences(sequences, x):
-    """(struct, number): None = one sequence of all rows; a 1-D integer tensor of n + 1 offsets; or a pair (begin, end) of n each."""
+def _sequences(sequences, x, zero_others):
+    """(struct, number): None = one sequence of all rows; a 1-D integer tensor of n + 1 offsets; or a pair (begin, end) of n each.
+    zero_others: rows of no sequence become zeros (else they are left as they were)."""
     if sequences is None:
-        return B.Sequences(1, None, None, 0), 1
+        return B.Sequences(1, None, None, 0, 0), 1
     pair = isinstance(sequences, (tuple, list))
     if pair and len(sequences) != 2:
         _refuse("sequences is not a tensor of offsets or a pair (begin, end)")
@@ -156,7 +157,7 @@ def _sequences(sequences, x):
         if n < 0:
             _refuse("sequences: offsets are one more than the sequences, at least one")
         pe = pb + size
-    return B.Sequences(n, pb, pe, size) if n else B.Sequences(0, None, None, 0), n
+    return B.Sequences(n, pb, pe, size, zero_others) if n else B.Sequences(0, None, None, 0, zero_others), n
 
 
 def _activation(name):
@@ -169,14 +170,14 @@ def gated_scan(gate, cand, sequences=None, *, h0=None, activation="none", last=F
     """h_t = (1 - z_t) h_{t-1} + z_t act(cand_t), z = sigmoid(gate), along every sequence: (h, last, carry).
 
     sequences: None (one sequence of all rows), n + 1 offsets, or a pair (begin, end), int32 or int64 on the GPU; rows of no sequence
-    are left as they were (in `out`; unspecified where the call makes h).  h0: the states in front of the first rows, (n, features)
+    are left as they were in `out`, and zeros where the call makes h.  h0: the states in front of the first rows, (n, features)
     float32, None = zeros.  last=True: the states behind the last rows, (n, features) float32, else None.  carry=True: what
     gated_scan_backward starts from, else None."""
     pg, sg = _rows("gate", gate)
     rows, hidden = shape = gate.shape
     pc, sc = _rows("cand", cand, gate, shape=shape)
     act = _activation(activation)
-    seq, n = _sequences(sequences, gate)
+    seq, n = _sequences(sequences, gate, out is None)
     h = _new(gate) if out is None else out
     ph, sh = _rows("out", h, gate, shape=shape)
     p0 = _floats("h0", h0, gate, n, hidden)
@@ -190,13 +191,14 @@ def gated_scan(gate, cand, sequences=None, *, h0=None, activation="none", last=F
 
 def gated_scan_backward(dh, gate, cand, carry, sequences=None, *, h0=None, dlast=None, activation="none", out=None):
     """(dgate, dcand, dh0) from the gradient of h (and of last: dlast), the inputs and the carry of
-    gated_scan(.., carry=True).  out: a pair of tensors for dgate and dcand."""
+    gated_scan(.., carry=True).  out: a pair of tensors for dgate and dcand, in which rows of no sequence are left as they were; where
+    the call makes them, the gradients of those rows are zeros."""
     pg, sg = _rows("gate", gate)
     rows, hidden = shape = gate.shape
     pc, sc = _rows("cand", cand, gate, shape=shape)
     pd, sd = _rows("dh", dh, gate, shape=shape)
     act = _activation(activation)
-    seq, n = _sequences(sequences, gate)
+    seq, n = _sequences(sequences, gate, out is None)
     dgate, dcand = out if out is not None else (_new(gate), _new(gate))
     po, so = _rows("dgate", dgate, gate, shape=shape)
     pq, sq = _rows("dcand", dcand, gate, shape=shape)

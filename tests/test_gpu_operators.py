@@ -347,6 +347,32 @@ def test_scan_keeps_other_sequences_apart():
     assert got[0][430 - 1].isnan().all()   # and inside a sequence a NaN stays one
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,hidden,s", [(300, 2, [0, 0, 5, 5, 200]), (128, 37, [3, 100]), (1000, 130, ([0, 128, 256, 300, 512], [100, 128, 299, 512, 630])),
+                                           (5, 24, [0]), (700, 70, [7]), (640, 64, [640, 640]), (3000, 20, [1, 2999])])
+def test_scan_makes_zeros_in_rows_of_no_sequence(dtype, rows, hidden, s):
+    """h and the gradients that a call makes itself: zeros in padding, whatever it and the memory held."""
+    seq = on_gpu(sequences_of(s, torch.int64))
+    n = len(s) - 1 if isinstance(s, list) else len(s[0])
+    gate, cand, h0, dh, dlast = scan_inputs(rows, hidden, n, dtype, seed=41)
+    m = inside(sequences_of(s, torch.int64), rows)
+    for t in (gate, cand, dh):
+        t[~m] = NAN
+    dirt = [torch.full((rows, hidden), NAN, dtype=dtype, device="cuda") for _ in range(8)]
+    out = [t.clone() for t in dirt[:3]]
+    del dirt   # what the calls are given next
+    h, last, carry = ops.gated_scan(*dev(gate, cand), seq, h0=h0.cuda(), last=True, carry=True)
+    dgate, dcand, dh0 = ops.gated_scan_backward(*dev(dh, gate, cand), carry, seq, h0=h0.cuda(), dlast=dlast.cuda())
+    for t in (h, dgate, dcand):
+        assert t.shape == (rows, hidden) and not t[~m].any() and not t[m].isnan().any()
+    # and in tensors of the caller's they are left alone, the others having the same bits
+    h2, last2, carry2 = ops.gated_scan(*dev(gate, cand), seq, h0=h0.cuda(), last=True, carry=True, out=out[0])
+    g2 = ops.gated_scan_backward(*dev(dh, gate, cand), carry, seq, h0=h0.cuda(), dlast=dlast.cuda(), out=out[1:])
+    for p, q in zip((h, dgate, dcand), (h2, g2[0], g2[1])):
+        assert q[~m].isnan().all() and same_bits(p[m], q[m])
+    assert same_bits(last, last2) and same_bits(dh0, g2[2])
+
+
 @pytest.mark.parametrize("lens", [[1536], [300, 1236], [64] * 24])
 @pytest.mark.parametrize("feature", [5, 64, 129])
 def test_scan_keeps_other_features_apart(feature, lens):

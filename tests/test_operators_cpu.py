@@ -119,6 +119,15 @@ def test_scan_backward_refusals():
     assert scan_backward(seq=(0, None, None, 0)) == B.AMP_OK
 
 
+def test_scan_rows_of_no_sequence_refusals():
+    refused(scan_forward(seq=(2, P + 3 * MB, P + 3 * MB + 4, 4, 2)), "zero_others")
+    refused(scan_backward(seq=(1, None, None, 0, -1)), "zero_others")
+    # without sequences every row is one to be zeroed: not a call that has nothing to do
+    refused(scan_forward(seq=(0, None, None, 0, 1), gate=None), "gate is NULL")
+    refused(scan_backward(seq=(0, None, None, 0, 1), dgate=None), "dgate is NULL")
+    assert scan_forward(seq=(0, None, None, 0, 1), h=None) == B.AMP_OK
+
+
 def test_scan_workspace_is_checked():
     n = ct.c_size_t()
     assert B.lib().amp_gated_scan_workspace(B.F32, 100000, 8, ct.byref(n)) == B.AMP_OK
