@@ -4,7 +4,9 @@ torch's current stream of the tensors' device, and a refused call raises binding
 
 Arrays are 2-D tensors (rows, features) on one GPU, torch.float32, bfloat16 or float16, features next to each other, any row stride;
 weights, states, statistics and losses are float32 and contiguous.  No call waits for the GPU or reads from it, so each can be captured
-into a HIP graph.  There is no autograd: a layer's backward pass is a call of its own, as in the rest of the library.
+into a HIP graph.  There is no autograd: a layer's backward pass is a call of its own, as in the rest of the library.  A tensor that
+requires grad is refused while grad mode is on, since its gradient would be lost (torch.no_grad(), detach(), or the forward and
+backward of a torch.autograd.Function); writes to a caller's tensor count as in-place changes of it.
 """
 from __future__ import annotations
 
@@ -30,6 +32,14 @@ def _refuse(msg):
     raise B.AmpError(B.AMP_EINVAL, msg)
 
 
+def _differentiated(name):
+    _refuse("%s requires grad, and no gradient would reach it: call under torch.no_grad() or with detach()" % name)
+
+
+# Tells torch's own autograd that a caller's tensor was written to.
+_written = torch.autograd.graph.increment_version
+
+
 def _check(rc):
     if rc:
         raise B.AmpError(rc, B.lib().amp_operator_error().decode())
@@ -52,6 +62,8 @@ def _rows(name, x, like=None, dtypes=DTYPES, shape=None):
     types, type) it has to share."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         _refuse("%s is not a 2-D tensor" % name)
+    if x.requires_grad and torch.is_grad_enabled():
+        _differentiated(name)
     if not x.is_cuda:
         _refuse("%s is not on a GPU" % name)
     if x.dtype not in dtypes:
@@ -75,6 +87,8 @@ def _floats(name, x, like, *shape):
         return None
     if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous() or x.get_device() != like.get_device():
         _refuse("%s is not a contiguous float32 tensor of shape %s on %s" % (name, shape, like.device))
+    if x.requires_grad and torch.is_grad_enabled():
+        _differentiated(name)
     return x.data_ptr()
 
 
@@ -113,6 +127,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, stats=False, out=None):
         mean = torch.empty(rows, dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
     _call(x, "amp_layer_norm_forward", DTYPES[x.dtype], rows, cols, px, sx, pw, pb, eps, py, sy, _ptr(mean), _ptr(rstd))
+    if out is not None:
+        _written(out)
     return (y, mean, rstd) if stats else y
 
 
@@ -132,6 +148,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, *, out=None):
     ws, n = _workspace("amp_layer_norm_workspace", x)
     _call(x, "amp_layer_norm_backward", DTYPES[x.dtype], rows, cols, pd, sd, px, sx, pw, pm, pr, po, so, dweight.data_ptr(), dbias.data_ptr(),
           _ptr(ws), n)
+    if out is not None:
+        _written(out)
     return dx, dweight, dbias
 
 
@@ -186,6 +204,8 @@ def gated_scan(gate, cand, sequences=None, *, h0=None, activation="none", last=F
     car = torch.empty((_size("amp_gated_scan_carry", dtype, rows, hidden), hidden), dtype=torch.float32, device=gate.device) if carry else None
     ws, nb = _workspace("amp_gated_scan_workspace", gate)
     _call(gate, "amp_gated_scan_forward", dtype, act, rows, hidden, pg, sg, pc, sc, ct.byref(seq), p0, ph, sh, _ptr(end), _ptr(car), _ptr(ws), nb)
+    if out is not None:
+        _written(out)
     return h, end, car
 
 
@@ -211,6 +231,8 @@ def gated_scan_backward(dh, gate, cand, carry, sequences=None, *, h0=None, dlast
     ws, nb = _workspace("amp_gated_scan_workspace", gate)
     _call(gate, "amp_gated_scan_backward", dtype, act, rows, hidden, pd, sd, pl, pg, sg, pc, sc, ct.byref(seq), p0, pk, po, so, pq, sq,
           dh0.data_ptr(), _ptr(ws), nb)
+    if out is not None:
+        _written((dgate, dcand))
     return dgate, dcand, dh0
 
 
@@ -227,6 +249,7 @@ def gated_scan_step(gate, cand, state, *, activation="none", out=None):
     h = _new(gate) if out is None else out
     ph, sh = _rows("out", h, gate, shape=shape)
     _call(gate, "amp_gated_scan_step", DTYPES[gate.dtype], _activation(activation), rows, hidden, pg, sg, pc, sc, ps, ss, ph, sh)
+    _written(state if out is None else (state, out))
     return h
 
 
@@ -256,4 +279,6 @@ def distill_loss(logits, teacher, index, temperature=1.0, weight=None, *, grad=T
     ws, nb = _workspace("amp_distill_workspace", logits)
     _call(logits, "amp_distill_loss", DTYPES[logits.dtype], rows, classes, px, sx, top, DTYPES[teacher.dtype], pt, st, pi, _INDEX[index.dtype],
           si, temperature, pw, loss.data_ptr(), pd, sd, _ptr(ws), nb)
+    if out is not None:
+        _written(out)
     return loss, dlogits

@@ -565,6 +565,59 @@ def test_wrappers_refuse():
             pytest.fail("call %d was taken" % k)
 
 
+def test_wrappers_and_autograd():
+    """Whatever requires grad is refused in grad mode, each argument of each call; without it the calls run, also inside a Function."""
+    def leaf(*shape):
+        return torch.rand(*shape, device="cuda", requires_grad=True)
+    x, w, st = torch.rand(4, 8, device="cuda"), torch.rand(8, device="cuda"), torch.rand(4, device="cuda")
+    i = torch.zeros(4, 3, dtype=torch.int64, device="cuda")
+    s, t = torch.rand(1, 8, device="cuda"), torch.rand(4, 3, device="cuda")
+    calls = [lambda: ops.layer_norm(leaf(4, 8)), lambda: ops.layer_norm(x, leaf(8)), lambda: ops.layer_norm(x, w, leaf(8)),
+             lambda: ops.layer_norm(x, out=leaf(4, 8)), lambda: ops.layer_norm_backward(leaf(4, 8), x, w, st, st),
+             lambda: ops.layer_norm_backward(x, leaf(4, 8), w, st, st), lambda: ops.layer_norm_backward(x, x, leaf(8), st, st),
+             lambda: ops.layer_norm_backward(x, x, w, leaf(4), st), lambda: ops.gated_scan(leaf(4, 8), x), lambda: ops.gated_scan(x, leaf(4, 8)),
+             lambda: ops.gated_scan(x, x, h0=leaf(1, 8)), lambda: ops.gated_scan_backward(leaf(4, 8), x, x, s),
+             lambda: ops.gated_scan_backward(x, x, leaf(4, 8), s), lambda: ops.gated_scan_backward(x, x, x, s, dlast=leaf(1, 8)),
+             lambda: ops.gated_scan_step(x, leaf(4, 8), x.clone()), lambda: ops.gated_scan_step(x, x, leaf(4, 8)),
+             lambda: ops.distill_loss(leaf(4, 8), t, i), lambda: ops.distill_loss(x, leaf(4, 3), i), lambda: ops.distill_loss(x, t, i, 1.0, leaf(4))]
+    for k, call in enumerate(calls):
+        with pytest.raises(B.AmpError, match="requires grad"):
+            call()
+            pytest.fail("call %d was taken" % k)
+        with torch.no_grad():
+            call()
+    # a tensor that is written to counts as changed: torch's own backward pass then says that it cannot use it
+    a, b, c = (torch.rand(4, 8, device="cuda") for _ in range(3))
+    for write in (lambda: ops.layer_norm(x, out=a), lambda: ops.layer_norm_backward(x, x, w, st, st, out=a),
+                  lambda: ops.gated_scan(x, x, out=a), lambda: ops.gated_scan_backward(x, x, x, s, out=(b, a)),
+                  lambda: ops.gated_scan_step(x, x, a), lambda: ops.gated_scan_step(x, x, c, out=a), lambda: ops.distill_loss(x, t, i, out=a)):
+        p = leaf(4, 8)
+        y = (p * a).sum()
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, b):
+            y, mean, rstd = ops.layer_norm(x, w, b, stats=True)
+            ctx.save_for_backward(x, w, mean, rstd)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return ops.layer_norm_backward(dy, *ctx.saved_tensors)
+    p, q, r, dy = leaf(5, 40), leaf(40), leaf(40), torch.rand(5, 40, device="cuda")
+    Norm.apply(p, q, r).backward(dy)
+    with torch.no_grad():
+        y, mean, rstd = ops.layer_norm(p, q, r, stats=True)
+        want = ops.layer_norm_backward(dy, p, q, mean, rstd)
+    assert all(same_bits(g.grad, v) for g, v in zip((p, q, r), want))
+    with torch.inference_mode():
+        z = torch.rand(4, 8, device="cuda")
+        ops.gated_scan_step(z, z, z.clone(), out=torch.empty_like(z))
+
+
 # ------------------------------------------------------------------ long and many
 def test_offsets_past_32_bits():
     """Rows so far apart that the last ones begin behind 2^32 elements: the bits of the same rows next to each other."""

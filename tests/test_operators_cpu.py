@@ -201,6 +201,18 @@ def test_wrappers_refuse_what_is_not_on_a_gpu():
         assert e.value.code == B.AMP_EINVAL
 
 
+def test_wrappers_refuse_tensors_that_require_grad():
+    """Checked before anything that needs a GPU; torch.no_grad() brings the call to the next check."""
+    x, g = torch.zeros(4, 8), torch.zeros(4, 8, requires_grad=True)
+    i = torch.zeros(4, 3, dtype=torch.int64)
+    for call in (lambda: ops.layer_norm(g), lambda: ops.layer_norm_backward(x, g, None, x[:, 0], x[:, 0]), lambda: ops.gated_scan(g, x),
+                 lambda: ops.gated_scan_backward(x, g, x, x), lambda: ops.gated_scan_step(g, x, x), lambda: ops.distill_loss(g, x[:, :3], i)):
+        with pytest.raises(B.AmpError, match="requires grad"):
+            call()
+        with torch.no_grad(), pytest.raises(B.AmpError, match="not on a GPU"):
+            call()
+
+
 # ------------------------------------------------------------------ the references against differences, in 64 bits
 def differences(f, x, eps=1e-6):
     g = torch.zeros_like(x)
