@@ -346,12 +346,14 @@ __global__ __launch_bounds__(TPB) void norm_dw_long_kernel(NormArgs a, int parts
   a.workspace[((size_t)blockIdx.y * 2 + 1) * a.cols + c] = b;
 }
 
-// The parts' sums, in their order within each of JOIN shares of them, and the shares': 32 columns to a workgroup.
+// The parts' sums, in their order within each of JOIN shares of them, and the shares': 32 columns to a workgroup.  A launch takes fewer
+// than 2^32 threads in a line (and starts fewer without an error where there are more), so the workgroups have several lines.
 constexpr int JOIN = 32;
+constexpr size_t JOIN_LINE = (size_t)1 << 20;
 __global__ __launch_bounds__(32 * JOIN) void norm_join_kernel(NormArgs a, int parts) {
   __shared__ float sum[JOIN][33];
   const int lane = threadIdx.x % 32, share = threadIdx.x / 32;
-  const size_t c = (size_t)blockIdx.x * 32 + lane, cols2 = 2 * a.cols;
+  const size_t c = ((size_t)blockIdx.y * JOIN_LINE + blockIdx.x) * 32 + lane, cols2 = 2 * a.cols;
   float s = 0.f;
   if (c < cols2)
     for (int p = share; p < parts; p += 8 * JOIN) {
@@ -452,7 +454,9 @@ extern "C" hipError_t amp_norm_backward_launch(int dtype, const NormArgs* a, hip
   const Shape s = shape_of(dtype, a->rows, a->cols, true);
   hipError_t e = hipSuccess;
   if (a->rows) OPS_BY_TYPE(dtype, e = backward<T>(s, a, stream));
-  if (e == hipSuccess && (a->dweight || a->dbias) && !(s.tpr && s.parts == 1))
-    e = launch(norm_join_kernel, dim3((unsigned)((2 * a->cols + 31) / 32)), dim3(32 * JOIN), 0, stream, *a, a->rows ? s.parts : 0);
+  if (e == hipSuccess && (a->dweight || a->dbias) && !(s.tpr && s.parts == 1)) {
+    const size_t groups = (2 * a->cols + 31) / 32, line = groups < JOIN_LINE ? groups : JOIN_LINE;
+    e = launch(norm_join_kernel, dim3((unsigned)line, (unsigned)((groups + line - 1) / line)), dim3(32 * JOIN), 0, stream, *a, a->rows ? s.parts : 0);
+  }
   return e;
 }

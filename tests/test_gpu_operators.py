@@ -153,6 +153,16 @@ def test_norm_far_from_zero_and_constant_rows(dtype):
     ref.check("rstd", rstd, want[2])
 
 
+@pytest.mark.parametrize("rows", [0, 2])
+def test_norm_of_more_columns_than_a_launch_joins_in_one_line(rows):
+    """The parameters' gradients of 2^26 columns and more; whole numbers, whose sums are exact in any order."""
+    cols = (1 << 26) + 3
+    x, dy = (torch.randint(-3, 4, (rows, cols), device="cuda", generator=torch.Generator("cuda").manual_seed(k)).bfloat16() for k in range(2))
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    dx, dw, db = ops.layer_norm_backward(dy, x, None, mean, rstd)
+    assert torch.equal(dw, (dy.float() * x.float()).sum(0)) and torch.equal(db, dy.float().sum(0))
+
+
 @pytest.mark.parametrize("cols", [37, 2048, 11111])
 def test_norm_keeps_other_rows_apart(cols):
     x, dy = rand(8, cols, seed=1), rand(8, cols, seed=2)
