@@ -153,6 +153,37 @@ def test_norm_far_from_zero_and_constant_rows(dtype):
     ref.check("rstd", rstd, want[2])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 40), (8, 24), (129, 5), (20000, 24), (4099, 37), (4000, 150), (513, 1000), (3001, 1021), (37, 2048), (2100, 2500),
+                                       (1037, 4099), (4097, 4096), (300, 11111), (2500, 8200), (17, 16400), (70, 20011), (600, 16400), (521, 33000)])
+def test_norm_parameter_gradients_count_every_row_once(dtype, rows, cols):
+    """Whole numbers and statistics that are powers of two: every sum is exact in 32 bits in whatever order (up to 20,000 terms of at
+    most 3 * 8 * 2, in halves: below 2^24), so that a row that is lost, doubled or given another's statistics shows."""
+    g = torch.Generator("cuda").manual_seed(rows + cols)
+    x, dy = (torch.randint(-3, 4, (rows, cols), device="cuda", generator=g).to(dtype) for _ in range(2))
+    mean = torch.randint(-5, 6, (rows,), device="cuda", generator=g).float()
+    rstd = 2.0 ** torch.randint(-1, 2, (rows,), device="cuda", generator=g).float()
+    for weight in (None, torch.ones(cols, device="cuda")):
+        dx, dw, db = ops.layer_norm_backward(dy, x, weight, mean, rstd)
+        n = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        assert torch.equal(dw.double(), (dy.double() * n).sum(0)) and torch.equal(db.double(), dy.double().sum(0))
+
+
+@pytest.mark.parametrize("dtype,cols", [(torch.float32, 16400), (torch.bfloat16, 33000)])
+def test_norm_more_long_rows_than_workgroups(dtype, cols):
+    """Rows that registers do not hold, more of them than a launch has workgroups: each as in a call of a few."""
+    rows = 4096 + 70
+    g = torch.Generator("cuda").manual_seed(7)
+    x, dy = (torch.randn(rows, cols, device="cuda", generator=g).to(dtype) for _ in range(2))
+    w, b = torch.randn(cols, device="cuda", generator=g), torch.randn(cols, device="cuda", generator=g)
+    y, mean, rstd = ops.layer_norm(x, w, b, stats=True)
+    dx = ops.layer_norm_backward(dy, x, w, mean, rstd)[0]
+    for s in (slice(0, 5), slice(60, 100), slice(rows - 75, rows)):
+        y2, mean2, rstd2 = ops.layer_norm(x[s], w, b, stats=True)
+        assert same_bits(y[s], y2) and same_bits(mean[s], mean2) and same_bits(rstd[s], rstd2)
+        assert same_bits(dx[s], ops.layer_norm_backward(dy[s], x[s], w, mean2, rstd2)[0])
+
+
 @pytest.mark.parametrize("rows", [0, 2])
 def test_norm_of_more_columns_than_a_launch_joins_in_one_line(rows):
     """The parameters' gradients of 2^26 columns and more; whole numbers, whose sums are exact in any order."""
