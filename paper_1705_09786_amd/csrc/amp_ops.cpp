@@ -254,11 +254,11 @@ int amp_gated_scan_backward(int dtype, int activation, size_t rows, size_t hidde
   const char* what = "gated_scan_backward";
   CHECK(check_scan(what, dtype, activation, rows, hidden, q));
   if (q->n == 0 && !q->zero_others) return AMP_OK;
+  REQUIRE(carry);   // which has a row where there are no others
   if (rows) {
     REQUIRE(dh);
     REQUIRE(gate);
     REQUIRE(cand);
-    REQUIRE(carry);
     REQUIRE(dgate);
     REQUIRE(dcand);
   }

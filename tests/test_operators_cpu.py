@@ -128,6 +128,15 @@ def test_scan_rows_of_no_sequence_refusals():
     assert scan_forward(seq=(0, None, None, 0, 1), h=None) == B.AMP_OK
 
 
+def test_scan_backward_without_rows_needs_the_carry():
+    """A call without rows starts its kernel too, for dh0, and the kernel reads a row of the carry."""
+    refused(scan_backward(rows=0, carry=None), "carry is NULL")
+    refused(scan_backward(rows=0, carry=None, dh=None, gate=None, cand=None, dgate=None, dcand=None, seq=(2, P + 6 * MB, P + 6 * MB + 4, 4)),
+            "carry is NULL")
+    n = ct.c_size_t()
+    assert B.lib().amp_gated_scan_carry(B.F32, 0, 8, ct.byref(n)) == B.AMP_OK and n.value == 1
+
+
 def test_scan_workspace_is_checked():
     n = ct.c_size_t()
     assert B.lib().amp_gated_scan_workspace(B.F32, 100000, 8, ct.byref(n)) == B.AMP_OK
