@@ -340,12 +340,13 @@ __device__ __forceinline__ void tile_map(const Maps<L>& m, int c, float& p, floa
 // those bits (a NaN is published as the one below).  The tiles of CH features are taken by ticket, in the order in which their states
 // follow each other (the backward pass: from the last on): a workgroup waits only for tiles that running workgroups have taken, so
 // every wait ends whatever else the GPU does.  (Another call writing the same workspace at the same time would break that: a wait
-// is given up after some seconds, and the states become NaN.)
+// is given up after WAIT_TURNS looks, some seconds, and the states become NaN.  Looks are counted, not time, which goes by as well while
+// the machine has the queue off the GPU.)
 constexpr int GROUP = 4;   // tiles that share a word
 constexpr int FAR = 16;    // groups in front that a wait looks at
 constexpr int AHEAD = 4;   // words of them on their way together
 constexpr unsigned EMPTY = 0xffffffffu, PUBLISHED_NAN = 0x7fc00000u;
-constexpr long WAIT_TICKS = 500000000;   // of the 100 MHz clock
+constexpr int WAIT_TURNS = 1 << 22;
 
 __device__ __forceinline__ unsigned long long word_of(float p, float q) {
   unsigned a = __float_as_uint(p), b = __float_as_uint(q);
@@ -399,8 +400,7 @@ __device__ __forceinline__ float hand_over(const Hand& h, size_t order, size_t s
   if (!closes) h.store(h.words, order, slot, p, q);
   float lp = 1.f, lq = 0.f, gp = p, gq = q, x = 0.f;   // the maps of the group's tiles in front, and with this one; what comes into the group
   bool local = r == 0, known = g == 0;
-  const long began = wall_clock64();
-  for (;;) {
+  for (int turn = 0;; ++turn) {
     unsigned long long w[GROUP - 1], next = 0, s = ~0ull;
     if (!local)
 #pragma unroll
@@ -457,7 +457,7 @@ __device__ __forceinline__ float hand_over(const Hand& h, size_t order, size_t s
       if (closes && !__all(is_cut(gp))) h.store(h.groups, g, slot, __uint_as_float(CUT), apply(gp, gq, x));
       return apply(lp, lq, x);
     }
-    if (wall_clock64() - began > WAIT_TICKS) {
+    if (turn == WAIT_TURNS) {
       if (closes) h.store(h.groups, g, slot, __uint_as_float(CUT), __uint_as_float(PUBLISHED_NAN));
       return __uint_as_float(PUBLISHED_NAN);
     }

@@ -1,6 +1,6 @@
 """The gated recurrence's maps and the hand-over of states between its tiles, taken from their source and compiled for the host: the 64
-lanes of a wave take turns from one meeting (ballot, vote) to the next.  Tiles run one after the other in the order of their tickets, so
-that everything a tile asks for is there when it asks: no wait may take a second turn, whatever the rows hold."""
+lanes of a wave take turns from one meeting (ballot, vote) to the next.  Where tiles run one after the other in the order of their tickets,
+everything a tile asks for is there when it asks: no wait may take a second turn, whatever the rows hold."""
 import ctypes as ct
 import os
 import re
@@ -27,15 +27,23 @@ static unsigned __float_as_uint(float f) { unsigned u; memcpy(&u, &f, 4); return
 struct ScanArgs { size_t hidden; void* workspace; };
 
 // ---- a wave: every lane runs up to the next meeting, then all of them go on with its result
-static ucontext_t g_main, g_lane[64];
-static unsigned long long g_vote, g_result;
-static int g_at, g_turns;
+struct Wave {
+  ucontext_t lane[64];
+  unsigned long long vote, result;
+  int turns;
+  size_t order;
+  float p[64], q[64], in[64];
+  bool done[64];
+};
+static ucontext_t g_main;
+static Wave* g_wave;
+static int g_at;
 static long g_clock;
 static struct { unsigned x; } threadIdx;
 static unsigned long long ballot(bool v) {
-  if (v) g_vote |= 1ull << g_at;
-  swapcontext(&g_lane[g_at], &g_main);
-  return g_result;
+  if (v) g_wave->vote |= 1ull << g_at;
+  swapcontext(&g_wave->lane[g_at], &g_main);
+  return g_wave->result;
 }
 #define __ballot(v) ballot(v)
 #define __all(v) (ballot(v) == ~0ull)
@@ -44,7 +52,7 @@ static unsigned long long ballot(bool v) {
 #define __hip_atomic_load(p, order, scope) (*(p))
 #define __hip_atomic_store(p, v, order, scope) (*(p) = (v))
 static long wall_clock64() { return g_clock; }
-#define __builtin_amdgcn_s_sleep(n) (g_turns += g_at == 63, g_clock += g_at == 63 ? WAIT_TICKS / 4 : 0)
+#define __builtin_amdgcn_s_sleep(n) (g_wave->turns += g_at == 63)
 constexpr int TILE = 128;
 %s
 
@@ -57,53 +65,59 @@ struct Flags {
 };
 %s
 
-// ---- a tile after the other
+// ---- the waves of several tiles, a turn each
 static const Hand* g_hand;
-static size_t g_order;
-static const float *g_p, *g_q;
-static float* g_in;
 static void lane_main() {
+  Wave& w = *g_wave;
   const int lane = g_at;
-  g_in[lane] = hand_over(*g_hand, g_order, 0, g_p[lane], g_q[lane]);
+  w.in[lane] = hand_over(*g_hand, w.order, 0, w.p[lane], w.q[lane]);
+  w.done[lane] = true;
 }
-static int run_tile(std::vector<char>& stacks) {
-  bool done[64] = {};
-  g_turns = 0;
+constexpr size_t STACK = 32768;
+static void start(Wave& w, char* stacks) {
+  w.vote = w.result = 0;
+  w.turns = 0;
   for (int l = 0; l < 64; ++l) {
-    getcontext(&g_lane[l]);
-    g_lane[l].uc_stack.ss_sp = &stacks[l * 65536];
-    g_lane[l].uc_stack.ss_size = 65536;
-    g_lane[l].uc_link = &g_main;
-    makecontext(&g_lane[l], lane_main, 0);
+    w.done[l] = false;
+    getcontext(&w.lane[l]);
+    w.lane[l].uc_stack.ss_sp = stacks + l * STACK;
+    w.lane[l].uc_stack.ss_size = STACK;
+    w.lane[l].uc_link = &g_main;
+    makecontext(&w.lane[l], lane_main, 0);
   }
-  for (int meeting = 0; meeting < 100000; ++meeting) {
-    g_vote = 0;
-    for (int l = 0; l < 64; ++l) {
-      g_at = l;
-      threadIdx.x = l;
-      g_in[l] = -12345.f;
-      swapcontext(&g_main, &g_lane[l]);
-      done[l] = g_in[l] != -12345.f;   // (a NaN is unequal too)
-    }
-    g_result = g_vote;
-    if (std::all_of(done, done + 64, [](bool d) { return d; })) return g_turns;
-    if (std::any_of(done, done + 64, [](bool d) { return d; })) return -1;   // lanes parted
+}
+// On to the wave's next meeting: 1 = all lanes are done, 0 = none, -1 = they parted.
+static int step(Wave& w) {
+  g_wave = &w;
+  w.vote = 0;
+  for (int l = 0; l < 64; ++l) {
+    g_at = l;
+    threadIdx.x = l;
+    swapcontext(&g_main, &w.lane[l]);
   }
-  return -2;
+  w.result = w.vote;
+  const int n = std::count(w.done, w.done + 64, true);
+  return n == 64 ? 1 : n ? -1 : 0;
 }
 
-// rows x 64 keeps, terms and flags (tiles * 128 rows, in the order of the states: back = 1 runs map_back over rows given from the first
-// on) -> what comes into every tile, and the extra turns of its wait
-extern "C" void run(int tiles, int back, const float* keep, const float* term, const unsigned char* flag, float* in, int* turns) {
-  std::vector<char> stacks(64 * 65536), ws(Hand::clear_bytes(tiles, 64) + 64 + tiles * 5 * TILE);
+// rows x 64 keeps, terms and flags (tiles * 128 rows from the first on; back = 1: the states run from the last on) -> what comes into
+// every tile, and the extra turns of its wait.  Up to `together` tiles are under way, the later ones first in every round of turns;
+// `jump` ticks of the clock go by between two rounds.
+extern "C" int run(int tiles, int back, int together, long jump, const float* keep, const float* term, const unsigned char* flag, float* in,
+                   int* turns) {
+  std::vector<char> ws(Hand::clear_bytes(tiles, 64) + 64 + tiles * 5 * TILE);
   memset(ws.data(), 0xff, ws.size());
   ScanArgs a = {64, ws.data()};
   const Hand hand(a, tiles);
   g_hand = &hand;
   g_clock = 0;
+  static std::vector<char> stacks;
+  stacks.resize(std::max(stacks.size(), together * 64 * STACK));
+  std::vector<Wave> waves(tiles);
   for (int order = 0; order < tiles; ++order) {
     const int tile = back ? tiles - 1 - order : order;
-    float p[64], q[64];
+    Wave& w = waves[order];
+    w.order = order;
     for (int c = 0; c < 64; c += 4) {
       float tp[4] = {1, 1, 1, 1}, tq[4] = {0, 0, 0, 0};
       for (int g = 0; g < TILE / 8; ++g) {
@@ -118,11 +132,22 @@ extern "C" void run(int tiles, int back, const float* keep, const float* term, c
           map_forward<false, Lay>(f, k, t, gp, gq);
         for (int j = 0; j < 4; ++j) compose(tp[j], tq[j], gp[j], gq[j]);
       }
-      for (int j = 0; j < 4; ++j) p[c + j] = tp[j], q[c + j] = tq[j];
+      for (int j = 0; j < 4; ++j) w.p[c + j] = tp[j], w.q[c + j] = tq[j];
     }
-    g_order = order, g_p = p, g_q = q, g_in = in + order * 64;
-    turns[order] = run_tile(stacks);
   }
+  for (int first = 0; first < tiles; first += together) {
+    const int end = std::min(tiles, first + together);
+    std::vector<int> state(end - first, 0);
+    for (int t = first; t < end; ++t) start(waves[t], stacks.data() + (t - first) * 64 * STACK);
+    for (int round = 0; std::count(state.begin(), state.end(), 1) < end - first; ++round) {
+      for (int t = end - 1; t >= first; --t)
+        if (!state[t - first] && (state[t - first] = step(waves[t])) < 0) return -1;
+      g_clock += jump;
+      if (round > 100000) return -2;
+    }
+  }
+  for (int t = 0; t < tiles; ++t) memcpy(in + t * 64, waves[t].in, sizeof waves[t].in), turns[t] = waves[t].turns;
+  return 0;
 }
 """
 
@@ -145,12 +170,13 @@ def hand_over(tmp_path_factory):
     assert p.returncode == 0, p.stdout
     lib = ct.CDLL(str(so))
 
-    def call(keep, term, flag, back):
+    def call(keep, term, flag, back, together=1, jump=0):
         tiles = keep.shape[0] // 128
         into, turns = np.zeros((tiles, 64), np.float32), np.zeros(tiles, np.int32)
         ptr = lambda a, t: np.ascontiguousarray(a).ctypes.data_as(ct.POINTER(t))
         keep, term, flag = np.ascontiguousarray(keep), np.ascontiguousarray(term), np.ascontiguousarray(flag)
-        lib.run(tiles, int(back), ptr(keep, ct.c_float), ptr(term, ct.c_float), ptr(flag, ct.c_uint8), ptr(into, ct.c_float), ptr(turns, ct.c_int))
+        assert lib.run(tiles, int(back), together, ct.c_long(jump), ptr(keep, ct.c_float), ptr(term, ct.c_float), ptr(flag, ct.c_uint8),
+                       ptr(into, ct.c_float), ptr(turns, ct.c_int)) == 0
         return into, turns
     return call
 
@@ -197,6 +223,19 @@ def test_states_are_the_serial_ones(hand_over, begins, back):
     # keeps of at most 1 and some 0.8 in the mean: a state is a sum of terms of size 4 at most over some 10 rows, each with the rounding
     # of its row and of up to 40 maps behind it
     assert np.abs(into - want).max() <= 2.0 ** -24 * 4 * 10 * 50
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("begins", [[0], [0, 700], [0, 5, 130, 390, 391, 900]])
+@pytest.mark.parametrize("together", [2, 3, 4, 5, TILES])
+def test_states_do_not_depend_on_who_comes_first(hand_over, begins, back, together):
+    """Tiles under way at once, the later ones ahead of those that they wait for: the same bits.  Also where minutes go by meanwhile, as
+    they do for a process whose queue the machine takes off the GPU: a wait is not given up for that."""
+    keep, term, flag = rows_of(begins, TILES * 128, seed=together)
+    want, _ = hand_over(keep, term, flag, back)
+    for jump in (0, 60 * 100000000):
+        got, turns = hand_over(keep, term, flag, back, together, jump)
+        assert (got.view(np.int32) == want.view(np.int32)).all() and turns.max() > 0
 
 
 @pytest.mark.parametrize("back", [False, True])
