@@ -365,8 +365,7 @@ struct Hand {
   int* seq;
   unsigned char* flag;
   size_t tiles, slots;   // slots: the features in whole workgroups
-  static constexpr int MOST_CH = 128;
-  __host__ __device__ static size_t slots_of(size_t hidden) { return (hidden + MOST_CH - 1) / MOST_CH * MOST_CH; }
+  __host__ __device__ static size_t slots_of(size_t hidden) { return (hidden + 63) / 64 * 64; }
   // a ticket counter for every 64 slots, words for all slots
   __host__ __device__ static size_t clear_bytes(size_t tiles, size_t hidden) { return slots_of(hidden) * (1 + (tiles + tiles / GROUP) * 8); }
   __device__ Hand(const ScanArgs& a, size_t tiles_) : tiles(tiles_), slots(slots_of(a.hidden)) {
