@@ -48,11 +48,14 @@ def _check(rc):
 def _call(x, name, *args):
     """A C call on the current stream of x's device, which is current during the call."""
     index, fn = x.get_device(), getattr(B.lib(), name)
-    if index == _current_device():
-        rc = fn(*args, _stream_of(index))
-    else:
-        with torch.cuda.device(index):
+    try:
+        if index == _current_device():
             rc = fn(*args, _stream_of(index))
+        else:
+            with torch.cuda.device(index):
+                rc = fn(*args, _stream_of(index))
+    except ct.ArgumentError as e:   # eps or temperature is no number
+        _refuse("%s: %s" % (name, e))
     if rc:
         _check(rc)
 
@@ -179,7 +182,7 @@ def _sequences(sequences, x, zero_others):
 
 
 def _activation(name):
-    if name not in ACTIVATIONS:
+    if not isinstance(name, str) or name not in ACTIVATIONS:
         _refuse("activation %r: none and tanh are taken" % (name,))
     return ACTIVATIONS[name]
 
@@ -219,6 +222,8 @@ def gated_scan_backward(dh, gate, cand, carry, sequences=None, *, h0=None, dlast
     pd, sd = _rows("dh", dh, gate, shape=shape)
     act = _activation(activation)
     seq, n = _sequences(sequences, gate, out is None)
+    if out is not None and not (isinstance(out, (tuple, list)) and len(out) == 2):
+        _refuse("out is not a pair of tensors")
     dgate, dcand = out if out is not None else (_new(gate), _new(gate))
     po, so = _rows("dgate", dgate, gate, shape=shape)
     pq, sq = _rows("dcand", dcand, gate, shape=shape)

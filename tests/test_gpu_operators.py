@@ -606,6 +606,20 @@ def test_wrappers_refuse():
             pytest.fail("call %d was taken" % k)
 
 
+def test_wrappers_refuse_arguments_of_other_kinds():
+    """What is no tensor, number or name where one is due is a refused call as well."""
+    x, st = torch.zeros(4, 8, device="cuda"), torch.zeros(4, device="cuda")
+    i, s = torch.zeros(4, 3, dtype=torch.int64, device="cuda"), torch.zeros(1, 8, device="cuda")
+    for call in (lambda: ops.layer_norm(x, eps="1"), lambda: ops.layer_norm(x, eps=None), lambda: ops.layer_norm(x, eps=st),
+                 lambda: ops.distill_loss(x, x[:, :3], i, st[0]), lambda: ops.distill_loss(x, x[:, :3], i, None),
+                 lambda: ops.gated_scan(x, x, activation=None), lambda: ops.gated_scan(x, x, activation=[]), lambda: ops.gated_scan(x, x, out=3),
+                 lambda: ops.gated_scan_backward(x, x, x, s, out=(x,)), lambda: ops.gated_scan_backward(x, x, x, s, out=torch.zeros(2, 4, 8, device="cuda")),
+                 lambda: ops.gated_scan_backward(x, x, x, s, out=5), lambda: ops.gated_scan(x, x, 4), lambda: ops.layer_norm(x, 2.0)):
+        with pytest.raises(B.AmpError) as e:
+            call()
+        assert e.value.code == B.AMP_EINVAL
+
+
 def test_wrappers_and_autograd():
     """Whatever requires grad is refused in grad mode, each argument of each call; without it the calls run, also inside a Function."""
     def leaf(*shape):
