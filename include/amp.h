@@ -490,8 +490,9 @@ int amp_measure_peaks(void *dev_buf, size_t bytes, void *hip_stream, double *lds
  *   - workspace: scratch memory of at least the bytes that the *_workspace
  *     call reports, 16-byte aligned, contents arbitrary before and after.
  *     Calls that may run at the same time (other streams, graphs replayed
- *     side by side) need workspaces of their own.  NULL where 0 bytes are
- *     needed.
+ *     side by side) need workspaces of their own: the kernels trust what they
+ *     wrote there, and calls that share one at the same time may go outside
+ *     their arrays.  NULL where 0 bytes are needed.
  *   - Errors: AMP_EINVAL for a bad argument, AMP_ENOMEM for too small a
  *     workspace, AMP_EDEVICE when a launch fails; amp_operator_error()
  *     returns the message of the calling thread's last failed call.
@@ -521,12 +522,15 @@ int amp_layer_norm_backward(int dtype, size_t rows, size_t cols, const void *dy,
 
 /* Sequences packed into the rows of an array: sequence s has the rows
  * begin[s] .. end[s] - 1.  begin and end are device arrays of n integers of
- * index_bytes (4 or 8) bytes, ascending and without overlap; end may be
- * begin + 1 of one array of n + 1 offsets.  Lengths of 0 are allowed, and so
- * are rows that belong to no sequence (padding, rows behind the last one):
- * their outputs (h, dgate, dcand) are left as they were, or set to zero with
- * zero_others = 1.  Bounds outside the rows are taken for the nearest row, and
- * outputs of sequences that overlap or descend are unspecified.  begin = end = NULL: one sequence (n = 1) of all rows. */
+ * index_bytes (4 or 8) bytes, in order: end[s] <= begin[s + 1], which holds
+ * for sequences of length 0 (begin[s] = end[s]) too: one that stands inside
+ * another is out of order.  end may be begin + 1 of one array of n + 1
+ * offsets.  Rows may belong to no sequence (padding, rows behind the last
+ * one): their outputs (h, dgate, dcand) are left as they were, or set to zero
+ * with zero_others = 1.  Bounds outside the rows are taken for the nearest
+ * row.  Outputs of sequences out of order are unspecified; no access leaves
+ * its array for them.  begin = end = NULL: one sequence (n = 1) of all rows.
+ */
 typedef struct amp_sequences {
   size_t n;
   const void *begin, *end;
@@ -543,7 +547,7 @@ typedef struct amp_sequences {
  * gets every row's state in the inputs' type; last (n x hidden floats, may be
  * NULL) the state behind every sequence's last row, h0 for an empty one.
  * carry (may be NULL): the states that the backward pass starts from,
- * amp_gated_scan_carry rows x hidden floats. */
+ * amp_gated_scan_carry rows x hidden floats (one row at least). */
 int amp_gated_scan_carry(int dtype, size_t rows, size_t hidden, size_t *carry_rows);
 int amp_gated_scan_workspace(int dtype, size_t rows, size_t hidden, size_t *bytes);   /* of either direction */
 int amp_gated_scan_forward(int dtype, int activation, size_t rows, size_t hidden, const void *gate, size_t gate_stride, const void *cand,

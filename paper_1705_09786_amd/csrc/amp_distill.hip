@@ -269,7 +269,8 @@ __global__ __launch_bounds__(TPB) void distill_kernel(DistillArgs a) {
   row_entries<TPB, false, T>(a, r, w, m, f, scale, dx, t);
 }
 
-// Longer rows than the registers hold.
+// Longer rows than the registers hold, above 131,072 classes of 16 bits or 65,536 of 32, are read twice: 2,048 x 152,000 bf16 325 us,
+// 1,024 x 128,000 f32 294 us, 1.35 and 1.45 times a copy of what they cannot do without.
 constexpr int LONG = 1024;
 template <class T>
 __global__ __launch_bounds__(LONG) void distill_long_kernel(DistillArgs a) {

@@ -339,9 +339,9 @@ __device__ __forceinline__ void tile_map(const Maps<L>& m, int c, float& p, floa
 // tiles and slot, then the rows' flags and sequences, the same for all features.  Counters and words are EMPTY before the kernel; no map has
 // those bits (a NaN is published as the one below).  The tiles of CH features are taken by ticket, in the order in which their states
 // follow each other (the backward pass: from the last on): a workgroup waits only for tiles that running workgroups have taken, so
-// every wait ends whatever else the GPU does.  (Another call writing the same workspace at the same time would break that: a wait
-// is given up after WAIT_TURNS looks, some seconds, and the states become NaN.  Looks are counted, not time, which goes by as well while
-// the machine has the queue off the GPU.)
+// every wait ends whatever else the GPU does.  (Another call that writes the same workspace at the same time, which amp.h forbids, could break
+// that: a wait is given up after WAIT_TURNS looks, some seconds, so that the GPU is free again, and the states become NaN.  Looks are
+// counted, not time, which goes by as well while the machine has the queue off the GPU.)
 constexpr int GROUP = 4;   // tiles that share a word
 constexpr int FAR = 16;    // groups in front that a wait looks at
 constexpr int AHEAD = 4;   // words of them on their way together
