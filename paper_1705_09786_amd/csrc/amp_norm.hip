@@ -4,7 +4,7 @@
 // stays in the registers of the threads that share it, mean and deviations are formed from there (deviations from the mean itself, not as a difference of two sums, which would lose what a mean
 // far from zero leaves), and the backward pass adds the parameters' gradients up in registers over all rows of a workgroup.
 // 32,768 x 4,096 bf16: 98 us forward (5.5 TB/s, a large copy's rate), 160 backward (5.0) and 4 that join the workgroups' parts;
-// 2,500 x 11,111 fp16, whose rows are not aligned to the groups they are read in: 33 us forward (3.4).  Longer rows are read three times
+// 2,500 x 11,111 fp16, whose rows are not aligned to the groups they are read in: 35 us forward (3.2).  Longer rows are read three times
 // in either direction: 4,096 x 40,000 bf16 takes 622 us forward and 845 backward, 5 and 4.4 times a copy of what they cannot do without.
 #include "amp_ops.hip.h"
 
@@ -378,8 +378,9 @@ __global__ __launch_bounds__(32 * JOIN) void norm_join_kernel(NormArgs a, int pa
 // Which kernel takes a row: the threads that share it and the 16-byte groups of each.  A wave to a row of up to 128 groups (256
 // forward) has no barriers; longer rows, and rows so few that a call is a latency (512 and fewer), have more threads.  The backward pass
 // keeps three values a column beside the row, so its threads have fewer groups: 2,500 x 11,111 fp16 takes 70 us on 1,024 threads of
-// two, 61 on 512 of four (forward 33 and 38).  Its workgroups, of which each leaves a part of the parameters' gradients to be read
-// again, have at least eight rows: 512 x 4,096 bf16 takes 27 us with a row to each, 2,048 x 4,096 43 us and 27 with eight.
+// two, 61 on 512 of four (forward, of inputs that the memory-side cache holds, 33 and 38).  Its workgroups, of which each leaves a part of
+// the parameters' gradients to be read again, have at least eight rows: 512 x 4,096 bf16 takes 27 us with a row to each, 2,048 x 4,096 43 us
+// and 27 with eight.
 struct Shape {
   int tpr, nv, parts;   // tpr = 0: longer than the registers hold; parts: workgroups of the backward pass
 };
