@@ -1,11 +1,12 @@
 // Layer norm, forward and backward (include/amp.h has the formulas).
 //
 // Both directions are bound by HBM: a row of up to 32,768 16-bit or 16,384 32-bit elements (16,384 of either backward) is read once and
-// stays in the registers of the threads that share it, mean and deviations are formed from there (deviations from the mean itself, not as a difference of two sums, which would lose what a mean
-// far from zero leaves), and the backward pass adds the parameters' gradients up in registers over all rows of a workgroup.
-// 32,768 x 4,096 bf16: 98 us forward (5.5 TB/s, a large copy's rate), 160 backward (5.0) and 4 that join the workgroups' parts;
-// 2,500 x 11,111 fp16, whose rows are not aligned to the groups they are read in: 35 us forward (3.2).  Longer rows are read three times
-// in either direction: 4,096 x 40,000 bf16 takes 622 us forward and 845 backward, 5 and 4.4 times a copy of what they cannot do without.
+// stays in the registers of the threads that share it, mean and deviations are formed from there (deviations from the mean itself, not
+// as a difference of two sums, which would lose what a mean far from zero leaves), and the backward pass adds the parameters' gradients
+// up in registers over all rows of a workgroup. 32,768 x 4,096 bf16: 98 us forward (5.5 TB/s, a large copy's rate), 160 backward (5.0)
+// and 4 that join the workgroups' parts; 2,500 x 11,111 fp16, whose rows are not aligned to the groups they are read in: 35 us forward
+// (3.2).  Longer rows are read three times in either direction: 4,096 x 40,000 bf16 takes 622 us forward and 845 backward, 5 and 4.4
+// times a copy of what they cannot do without.
 #include "amp_ops.hip.h"
 
 namespace {
