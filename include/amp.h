@@ -588,6 +588,55 @@ int amp_distill_loss(int dtype, size_t rows, size_t classes, const void *logits,
                      float temperature, const float *weight, float *loss, void *dlogits, size_t dlogits_stride, void *workspace,
                      size_t workspace_bytes, void *hip_stream);
 
+/* The gated delta rule: a recurrence whose state is a matrix S of dk x dv
+ * (keys by values) for every sequence and head, which a row corrects at its
+ * key instead of adding to it.  Per head, with a_t = e^decay_t:
+ *   e_t = v_t - (a_t S_{t-1})^T k_t,  S_t = a_t S_{t-1} + beta_t k_t e_t^T,
+ *   o_t = scale S_t^T q_t
+ * q and k: rows of key_heads x dk elements, v and o: rows of heads x dv, decay
+ * and beta: rows of heads floats, all with strides of their own, so that they
+ * may be columns of one wider array.  key_heads divides heads; head h reads
+ * the keys and queries of key head h / (heads / key_heads).  States are
+ * n x heads x dk x dv floats.  Meant for keys of length about one, beta in
+ * 0 .. 2 and decays of at most 0 (-infinity forgets the state), where errors
+ * do not grow; other values are taken as the formula has them.  A value that
+ * is not finite may reach every row of its sequence and head, none of others.
+ * dk 1 .. 128, dv 1 .. 1024, heads below 2^16, fewer than 2^30 rows; at most
+ * 2^22 of (rows / 64 + sequences) x heads.
+ *
+ * h0 (may be NULL = zeros): states in front of the first rows.  last (may be
+ * NULL): states behind the last rows, h0 for an empty sequence.  carry (may be
+ * NULL): what the backward pass starts from, as many floats as
+ * amp_gated_delta_carry says.  o may be NULL.  sequences: as in the gated
+ * linear recurrence; with zero_others the rows of no sequence become zeros in
+ * o and in the backward pass's five outputs by row. */
+typedef struct amp_delta_shape {
+  int32_t dtype;   /* of q, k, v, o and their gradients */
+  size_t rows, heads, key_heads, dk, dv;
+} amp_delta_shape;
+int amp_gated_delta_carry(const amp_delta_shape *shape, size_t n_sequences, size_t *floats);
+int amp_gated_delta_workspace(const amp_delta_shape *shape, size_t n_sequences, int backward, size_t *bytes);
+int amp_gated_delta_forward(const amp_delta_shape *shape, const void *q, size_t q_stride, const void *k, size_t k_stride, const void *v,
+                            size_t v_stride, const float *decay, size_t decay_stride, const float *beta, size_t beta_stride, float scale,
+                            const amp_sequences *sequences, const float *h0, void *o, size_t o_stride, float *last, float *carry,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Its gradients.  dout: gradient of o; dlast (may be NULL): of the last
+ * states; carry: as the forward pass left it for the same inputs.  dq and dk
+ * are sums over the heads that share a key head.  dh0 (may be NULL): dlast
+ * (or 0) for an empty sequence. */
+int amp_gated_delta_backward(const amp_delta_shape *shape, const void *dout, size_t dout_stride, const float *dlast, const void *q,
+                             size_t q_stride, const void *k, size_t k_stride, const void *v, size_t v_stride, const float *decay,
+                             size_t decay_stride, const float *beta, size_t beta_stride, float scale, const amp_sequences *sequences,
+                             const float *carry, void *dq, size_t dq_stride, void *dk, size_t dk_stride, void *dv, size_t dv_stride,
+                             float *ddecay, size_t ddecay_stride, float *dbeta, size_t dbeta_stride, float *dh0, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+/* One row of each of shape->rows sequences: the states (state_stride floats
+ * apart, heads x dk x dv floats each) are brought up to date in place, o (may
+ * be NULL) gets the rows' outputs. */
+int amp_gated_delta_step(const amp_delta_shape *shape, const void *q, size_t q_stride, const void *k, size_t k_stride, const void *v,
+                         size_t v_stride, const float *decay, size_t decay_stride, const float *beta, size_t beta_stride, float scale,
+                         float *state, size_t state_stride, void *o, size_t o_stride, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -71,8 +71,14 @@ class Sequences(ct.Structure):
                 ("zero_others", ct.c_int32)]
 
 
+class DeltaShape(ct.Structure):
+    _fields_ = [("dtype", ct.c_int32), ("rows", ct.c_size_t), ("heads", ct.c_size_t), ("key_heads", ct.c_size_t), ("dk", ct.c_size_t),
+                ("dv", ct.c_size_t)]
+
+
 _ctxp = ct.c_void_p
 _i, _n, _p, _f = ct.c_int, ct.c_size_t, ct.c_void_p, ct.c_float   # operators' arguments: int, size or stride, device pointer, float
+_rows5 = [_p, _n] * 5   # q, k, v, decay, beta with their strides
 SIGNATURES = {
     "amp_create": (ct.c_int, [ct.POINTER(_ctxp), ct.c_void_p, ct.c_size_t, ct.c_void_p]),
     "amp_create_static": (ct.c_int, [ct.POINTER(_ctxp), ct.c_void_p]),
@@ -133,6 +139,12 @@ SIGNATURES = {
     "amp_gated_scan_backward": (_i, [_i, _i, _n, _n, _p, _n, _p, _p, _n, _p, _n, ct.POINTER(Sequences), _p, _p, _p, _n, _p, _n, _p, _p,
                                      _n, _p]),
     "amp_gated_scan_step": (_i, [_i, _i, _n, _n, _p, _n, _p, _n, _p, _n, _p, _n, _p]),
+    "amp_gated_delta_carry": (_i, [ct.POINTER(DeltaShape), _n, ct.POINTER(_n)]),
+    "amp_gated_delta_workspace": (_i, [ct.POINTER(DeltaShape), _n, _i, ct.POINTER(_n)]),
+    "amp_gated_delta_forward": (_i, [ct.POINTER(DeltaShape)] + _rows5 + [_f, ct.POINTER(Sequences), _p, _p, _n, _p, _p, _p, _n, _p]),
+    "amp_gated_delta_backward": (_i, [ct.POINTER(DeltaShape), _p, _n, _p] + _rows5 + [_f, ct.POINTER(Sequences), _p] + _rows5 +
+                                 [_p, _p, _n, _p]),
+    "amp_gated_delta_step": (_i, [ct.POINTER(DeltaShape)] + _rows5 + [_f, _p, _n, _p, _n, _p]),
     "amp_distill_workspace": (_i, [_i, _n, _n, ct.POINTER(_n)]),
     "amp_distill_loss": (_i, [_i, _n, _n, _p, _n, _n, _i, _p, _n, _p, _i, _n, _f, _p, _p, _p, _n, _p, _n, _p]),
 }

@@ -115,10 +115,7 @@ int check_scan_stride(const char* what, const char* name, size_t stride) {
   return stride < (size_t)1 << 22 ? AMP_OK : fail(AMP_EINVAL, "%s: %s has a row stride of 2^22 or more", what, name);
 }
 
-int check_scan(const char* what, int dtype, int activation, size_t rows, size_t hidden, const amp_sequences* q) {
-  CHECK(check_scan_size(what, dtype, rows, hidden));
-  if (activation != AMP_ACT_NONE && activation != AMP_ACT_TANH)
-    return fail(AMP_EINVAL, "%s: activation %d, AMP_ACT_NONE and AMP_ACT_TANH are taken", what, activation);
+int check_sequences(const char* what, const amp_sequences* q) {
   if (!q) return fail(AMP_EINVAL, "%s: sequences is NULL", what);
   if (q->n >= MAX_ROWS) return fail(AMP_EINVAL, "%s: %zu sequences, fewer than 2^31 are taken", what, q->n);
   if (q->zero_others != 0 && q->zero_others != 1) return fail(AMP_EINVAL, "%s: zero_others %d, 0 and 1 are taken", what, q->zero_others);
@@ -133,10 +130,51 @@ int check_scan(const char* what, int dtype, int activation, size_t rows, size_t 
   return AMP_OK;
 }
 
+int check_scan(const char* what, int dtype, int activation, size_t rows, size_t hidden, const amp_sequences* q) {
+  CHECK(check_scan_size(what, dtype, rows, hidden));
+  if (activation != AMP_ACT_NONE && activation != AMP_ACT_TANH)
+    return fail(AMP_EINVAL, "%s: activation %d, AMP_ACT_NONE and AMP_ACT_TANH are taken", what, activation);
+  return check_sequences(what, q);
+}
+
 #define REQUIRE(p)                                                              \
   do {                                                                          \
     if (!(p)) return fail(AMP_EINVAL, "%s: %s is NULL", what, #p);              \
   } while (0)
+
+int check_delta_shape(const char* what, const amp_delta_shape* s, size_t n) {
+  if (!s) return fail(AMP_EINVAL, "%s: shape is NULL", what);
+  if (s->dtype < AMP_F32 || s->dtype > AMP_F16) return fail(AMP_EINVAL, "%s: unknown dtype %d", what, s->dtype);
+  if (s->rows >= MAX_ROWS / 2) return fail(AMP_EINVAL, "%s: %zu rows, fewer than 2^30 are taken", what, s->rows);
+  if (s->heads < 1 || s->heads >= (size_t)1 << 16) return fail(AMP_EINVAL, "%s: heads = %zu, 1 .. 65535 are taken", what, s->heads);
+  if (s->key_heads < 1 || s->key_heads > s->heads || s->heads % s->key_heads)
+    return fail(AMP_EINVAL, "%s: key_heads = %zu does not divide heads = %zu", what, s->key_heads, s->heads);
+  if (s->dk < 1 || s->dk > DELTA_MAX_KEY) return fail(AMP_EINVAL, "%s: dk = %zu, 1 .. %d are taken", what, s->dk, DELTA_MAX_KEY);
+  if (s->dv < 1 || s->dv > 1024) return fail(AMP_EINVAL, "%s: dv = %zu, 1 .. 1024 are taken", what, s->dv);
+  if (n >= MAX_ROWS) return fail(AMP_EINVAL, "%s: %zu sequences, fewer than 2^31 are taken", what, n);
+  // a launch has fewer than 2^32 threads, a workgroup to a block or a sequence, and a head
+  if ((s->rows / DELTA_BLOCK + n) * s->heads > (size_t)1 << 22)
+    return fail(AMP_EINVAL, "%s: %zu rows in %zu sequences of %zu heads, up to 2^22 of (rows / %d + sequences) heads are taken", what, s->rows, n,
+                s->heads, DELTA_BLOCK);
+  return AMP_OK;
+}
+
+// What the calls of the delta rule have in common, in front of their outputs.
+struct DeltaIn {
+  const void* p;
+  size_t stride;
+};
+void delta_in(DeltaArgs& a, const amp_delta_shape* s, const DeltaIn& q, const DeltaIn& k, const DeltaIn& v, const DeltaIn& decay, const DeltaIn& beta,
+              float scale, const amp_sequences* seq) {
+  a.rows = s->rows, a.heads = (int)s->heads, a.key_heads = (int)s->key_heads, a.dk = (int)s->dk, a.dv = (int)s->dv;
+  a.q = q.p, a.q_stride = q.stride, a.k = k.p, a.k_stride = k.stride, a.v = v.p, a.v_stride = v.stride;
+  a.decay = (const float*)decay.p, a.decay_stride = decay.stride, a.beta = (const float*)beta.p, a.beta_stride = beta.stride, a.scale = scale;
+  a.n_seq = seq->n, a.begin = seq->begin, a.end = seq->end, a.index_bytes = seq->index_bytes, a.zero_others = seq->zero_others;
+}
+
+size_t delta_carry_floats(const amp_delta_shape* s, size_t n) {
+  return s->rows * s->heads * s->dv + amp_delta_blocks(s->rows, n) * s->heads * s->dk * s->dv;
+}
 
 }  // namespace
 
@@ -304,6 +342,133 @@ int amp_gated_scan_step(int dtype, int activation, size_t rows, size_t hidden, c
   a.rows = rows, a.hidden = hidden, a.gate = gate, a.gate_stride = gate_stride, a.cand = cand, a.cand_stride = cand_stride;
   a.state = state, a.state_stride = state_stride, a.h = h, a.h_stride = h_stride;
   return launched(what, amp_scan_step_launch(dtype, activation == AMP_ACT_TANH, &a, (hipStream_t)hip_stream));
+}
+
+int amp_gated_delta_carry(const amp_delta_shape* s, size_t n, size_t* floats) {
+  const char* what = "gated_delta_carry";
+  CHECK(check_delta_shape(what, s, n));
+  REQUIRE(floats);
+  *floats = delta_carry_floats(s, n);
+  return AMP_OK;
+}
+
+int amp_gated_delta_workspace(const amp_delta_shape* s, size_t n, int backward, size_t* bytes) {
+  const char* what = "gated_delta_workspace";
+  CHECK(check_delta_shape(what, s, n));
+  REQUIRE(bytes);
+  *bytes = amp_delta_workspace_bytes(s->rows, n, s->heads, s->dk, s->dv, backward);
+  return AMP_OK;
+}
+
+int amp_gated_delta_forward(const amp_delta_shape* shape, const void* q, size_t q_stride, const void* k, size_t k_stride, const void* v,
+                            size_t v_stride, const float* decay, size_t decay_stride, const float* beta, size_t beta_stride, float scale,
+                            const amp_sequences* seq, const float* h0, void* o, size_t o_stride, float* last, float* carry, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  const char* what = "gated_delta_forward";
+  CHECK(check_sequences(what, seq));
+  CHECK(check_delta_shape(what, shape, seq->n));
+  const size_t rows = shape->rows, heads = shape->heads, n = seq->n, ib = seq->index_bytes;
+  if ((n == 0 && !seq->zero_others) || (!o && !last && !carry)) return AMP_OK;
+  if (rows) {
+    REQUIRE(q);
+    REQUIRE(k);
+    REQUIRE(v);
+    REQUIRE(decay);
+    REQUIRE(beta);
+  }
+  const size_t e = elem(shape->dtype), keys = shape->key_heads * shape->dk, values = heads * shape->dv, state = heads * shape->dk * shape->dv;
+  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->dk, shape->dv, 0), nc = delta_carry_floats(shape, n);
+  const Span s[] = {{"o", o, rows, values, o_stride, e},          {"last", last, n, state, state, 4},
+                    {"carry", carry, 1, nc, nc, 4},               {"workspace", need ? workspace : nullptr, 1, need, need, 1},
+                    {"q", q, rows, keys, q_stride, e},            {"k", k, rows, keys, k_stride, e},
+                    {"v", v, rows, values, v_stride, e},          {"decay", decay, rows, heads, decay_stride, 4},
+                    {"beta", beta, rows, heads, beta_stride, 4},  {"h0", h0, n, state, state, 4},
+                    {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
+  CHECK(check_arrays(what, s, 4));
+  CHECK(check_workspace(what, workspace, workspace_bytes, need));
+  CHECK(check_overlaps(what, s, 4, nullptr, 0));
+  DeltaArgs a = {};
+  delta_in(a, shape, {q, q_stride}, {k, k_stride}, {v, v_stride}, {decay, decay_stride}, {beta, beta_stride}, scale, seq);
+  a.h0 = h0, a.o = o, a.o_stride = o_stride, a.last = last, a.carry = carry, a.workspace = workspace;
+  a.zero[0] = {o, o_stride * e, values * e / 2};
+  return launched(what, amp_delta_forward_launch(shape->dtype, &a, (hipStream_t)hip_stream));
+}
+
+int amp_gated_delta_backward(const amp_delta_shape* shape, const void* dout, size_t dout_stride, const float* dlast, const void* q,
+                             size_t q_stride, const void* k, size_t k_stride, const void* v, size_t v_stride, const float* decay,
+                             size_t decay_stride, const float* beta, size_t beta_stride, float scale, const amp_sequences* seq,
+                             const float* carry, void* dq, size_t dq_stride, void* dk, size_t dk_stride, void* dv, size_t dv_stride,
+                             float* ddecay, size_t ddecay_stride, float* dbeta, size_t dbeta_stride, float* dh0, void* workspace,
+                             size_t workspace_bytes, void* hip_stream) {
+  const char* what = "gated_delta_backward";
+  CHECK(check_sequences(what, seq));
+  CHECK(check_delta_shape(what, shape, seq->n));
+  const size_t rows = shape->rows, heads = shape->heads, n = seq->n, ib = seq->index_bytes;
+  if (n == 0 && !seq->zero_others) return AMP_OK;
+  if (rows) {
+    REQUIRE(dout);
+    REQUIRE(q);
+    REQUIRE(k);
+    REQUIRE(v);
+    REQUIRE(decay);
+    REQUIRE(beta);
+    REQUIRE(carry);
+    REQUIRE(dq);
+    REQUIRE(dk);
+    REQUIRE(dv);
+    REQUIRE(ddecay);
+    REQUIRE(dbeta);
+  }
+  const size_t e = elem(shape->dtype), keys = shape->key_heads * shape->dk, values = heads * shape->dv, state = heads * shape->dk * shape->dv;
+  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->dk, shape->dv, 1), nc = delta_carry_floats(shape, n);
+  const Span s[] = {{"dq", dq, rows, keys, dq_stride, e},               {"dk", dk, rows, keys, dk_stride, e},
+                    {"dv", dv, rows, values, dv_stride, e},             {"ddecay", ddecay, rows, heads, ddecay_stride, 4},
+                    {"dbeta", dbeta, rows, heads, dbeta_stride, 4},     {"dh0", dh0, n, state, state, 4},
+                    {"workspace", need ? workspace : nullptr, 1, need, need, 1},
+                    {"dout", dout, rows, values, dout_stride, e},       {"q", q, rows, keys, q_stride, e},
+                    {"k", k, rows, keys, k_stride, e},                  {"v", v, rows, values, v_stride, e},
+                    {"decay", decay, rows, heads, decay_stride, 4},     {"beta", beta, rows, heads, beta_stride, 4},
+                    {"carry", carry, 1, nc, nc, 4},                     {"dlast", dlast, n, state, state, 4},
+                    {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
+  CHECK(check_arrays(what, s, 7));
+  CHECK(check_workspace(what, workspace, workspace_bytes, need));
+  CHECK(check_overlaps(what, s, 7, nullptr, 0));
+  DeltaArgs a = {};
+  delta_in(a, shape, {q, q_stride}, {k, k_stride}, {v, v_stride}, {decay, decay_stride}, {beta, beta_stride}, scale, seq);
+  a.dout = dout, a.dout_stride = dout_stride, a.dlast = dlast, a.carry_in = carry, a.workspace = workspace;
+  a.dq = dq, a.dq_stride = dq_stride, a.dkey = dk, a.dk_stride = dk_stride, a.dvalue = dv, a.dv_stride = dv_stride;
+  a.ddecay = ddecay, a.ddecay_stride = ddecay_stride, a.dbeta = dbeta, a.dbeta_stride = dbeta_stride, a.dh0 = dh0;
+  a.zero[0] = {dq, dq_stride * e, keys * e / 2}, a.zero[1] = {dk, dk_stride * e, keys * e / 2}, a.zero[2] = {dv, dv_stride * e, values * e / 2};
+  a.zero[3] = {ddecay, ddecay_stride * 4, heads * 2}, a.zero[4] = {dbeta, dbeta_stride * 4, heads * 2};
+  return launched(what, amp_delta_backward_launch(shape->dtype, &a, (hipStream_t)hip_stream));
+}
+
+int amp_gated_delta_step(const amp_delta_shape* shape, const void* q, size_t q_stride, const void* k, size_t k_stride, const void* v,
+                         size_t v_stride, const float* decay, size_t decay_stride, const float* beta, size_t beta_stride, float scale,
+                         float* state, size_t state_stride, void* o, size_t o_stride, void* hip_stream) {
+  const char* what = "gated_delta_step";
+  CHECK(check_delta_shape(what, shape, 0));
+  const size_t rows = shape->rows, heads = shape->heads, e = elem(shape->dtype);
+  if (rows == 0) return AMP_OK;
+  if (rows * heads > (size_t)1 << 22) return fail(AMP_EINVAL, "%s: %zu rows of %zu heads, up to 2^22 are taken", what, rows, heads);
+  REQUIRE(q);
+  REQUIRE(k);
+  REQUIRE(v);
+  REQUIRE(decay);
+  REQUIRE(beta);
+  REQUIRE(state);
+  const size_t keys = shape->key_heads * shape->dk, values = heads * shape->dv;
+  const Span s[] = {{"state", state, rows, heads * shape->dk * shape->dv, state_stride, 4}, {"o", o, rows, values, o_stride, e},
+                    {"q", q, rows, keys, q_stride, e},            {"k", k, rows, keys, k_stride, e},
+                    {"v", v, rows, values, v_stride, e},          {"decay", decay, rows, heads, decay_stride, 4},
+                    {"beta", beta, rows, heads, beta_stride, 4}};
+  CHECK(check_arrays(what, s, 2));
+  CHECK(check_overlaps(what, s, 2, nullptr, 0));
+  DeltaStepArgs a = {};
+  a.rows = rows, a.heads = (int)heads, a.key_heads = (int)shape->key_heads, a.dk = (int)shape->dk, a.dv = (int)shape->dv;
+  a.q = q, a.q_stride = q_stride, a.k = k, a.k_stride = k_stride, a.v = v, a.v_stride = v_stride, a.decay = decay, a.decay_stride = decay_stride;
+  a.beta = beta, a.beta_stride = beta_stride, a.scale = scale, a.state = state, a.state_stride = state_stride, a.o = o, a.o_stride = o_stride;
+  return launched(what, amp_delta_step_launch(shape->dtype, &a, (hipStream_t)hip_stream));
 }
 
 int amp_distill_workspace(int dtype, size_t rows, size_t classes, size_t* bytes) {

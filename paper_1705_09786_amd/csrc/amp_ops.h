@@ -58,6 +58,54 @@ struct DistillArgs {
 
 #define OPS_MAX_TOP 1024
 
+#define DELTA_CHUNK 32   // rows whose errors are solved for together
+#define DELTA_BLOCK 64   // rows between two states that the backward pass starts from
+#define DELTA_MAX_KEY 128
+
+struct DeltaZero {   // an output whose rows of no sequence become zeros: bytes between rows, 16-bit halves of a row
+  void* p;
+  size_t stride, halves;
+};
+
+struct DeltaArgs {
+  size_t rows, n_seq;
+  int heads, key_heads, dk, dv;
+  const void *q, *k, *v, *dout;
+  size_t q_stride, k_stride, v_stride, dout_stride;
+  const float *decay, *beta;
+  size_t decay_stride, beta_stride;
+  float scale;
+  int index_bytes, zero_others;
+  const void *begin, *end;
+  const float *h0, *dlast, *carry_in;
+  void *o, *dq, *dkey, *dvalue;
+  size_t o_stride, dq_stride, dk_stride, dv_stride;
+  float *ddecay, *dbeta;
+  size_t ddecay_stride, dbeta_stride;
+  float *last, *dh0, *carry;
+  void* workspace;
+  DeltaZero zero[5];
+  // set by the launchers: the workspace's parts, and where the carry's states begin
+  size_t blocks, carry_states;
+  int* first;
+  float *matrices, *x, *behind;
+  double* sums;
+};
+
+struct DeltaStepArgs {
+  size_t rows;
+  int heads, key_heads, dk, dv;
+  const void *q, *k, *v;
+  size_t q_stride, k_stride, v_stride;
+  const float *decay, *beta;
+  size_t decay_stride, beta_stride;
+  float scale;
+  float* state;
+  size_t state_stride;
+  void* o;
+  size_t o_stride;
+};
+
 extern "C" {
 size_t amp_norm_workspace_bytes(int dtype, size_t rows, size_t cols);
 hipError_t amp_norm_forward_launch(int dtype, const NormArgs* a, hipStream_t stream);
@@ -67,6 +115,11 @@ size_t amp_scan_workspace_bytes(int dtype, size_t rows, size_t hidden);
 hipError_t amp_scan_forward_launch(int dtype, int tanh, const ScanArgs* a, hipStream_t stream);
 hipError_t amp_scan_backward_launch(int dtype, int tanh, const ScanArgs* a, hipStream_t stream);
 hipError_t amp_scan_step_launch(int dtype, int tanh, const ScanStepArgs* a, hipStream_t stream);
+size_t amp_delta_blocks(size_t rows, size_t n);
+size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, int backward);
+hipError_t amp_delta_forward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
+hipError_t amp_delta_backward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
+hipError_t amp_delta_step_launch(int dtype, const DeltaStepArgs* a, hipStream_t stream);
 size_t amp_distill_workspace_bytes(int dtype, size_t rows, size_t classes);
 hipError_t amp_distill_launch(int dtype, const DistillArgs* a, hipStream_t stream);
 }

@@ -258,6 +258,113 @@ def gated_scan_step(gate, cand, state, *, activation="none", out=None):
     return h
 
 
+# ------------------------------------------------------------------ gated delta rule
+@lru_cache(maxsize=4096)
+def _delta_shape(dtype, rows, heads, key_heads, dk, dv):
+    return B.DeltaShape(dtype, rows, heads, key_heads, dk, dv)
+
+
+@lru_cache(maxsize=4096)
+def _delta_sizes(dtype, rows, heads, key_heads, dk, dv, n):
+    """Floats of the carry, bytes of either direction's workspace."""
+    shape, out, x = _delta_shape(dtype, rows, heads, key_heads, dk, dv), [], ct.c_size_t()
+    _check(B.lib().amp_gated_delta_carry(ct.byref(shape), n, ct.byref(x)))
+    out.append(x.value)
+    for backward in (0, 1):
+        _check(B.lib().amp_gated_delta_workspace(ct.byref(shape), n, backward, ct.byref(x)))
+        out.append(x.value)
+    return out
+
+
+def _delta_inputs(q, k, v, decay, beta, key_heads, scale):
+    """(the sizes, their arguments in a C call)."""
+    pq, sq = _rows("q", q)
+    rows, keys = shape = q.shape
+    pk, sk = _rows("k", k, q, shape=shape)
+    pv, sv = _rows("v", v, q)
+    pd, sd = _rows("decay", decay, q, _FLOAT_ROWS)
+    heads, values = decay.size(1), v.size(1)
+    pb, sb = _rows("beta", beta, q, _FLOAT_ROWS, decay.shape)
+    if v.size(0) != rows or decay.size(0) != rows:
+        _refuse("q, v and decay have %d, %d and %d rows" % (rows, v.size(0), decay.size(0)))
+    if key_heads is None:
+        key_heads = heads
+    if not isinstance(key_heads, int) or key_heads < 1 or heads < 1 or keys % key_heads or values % heads:
+        _refuse("%d features of q in %r key heads, %d of v in %d heads" % (keys, key_heads, values, heads))
+    dk = keys // key_heads
+    sizes = (DTYPES[q.dtype], rows, heads, key_heads, dk, values // heads)
+    if scale is None:
+        scale = dk ** -0.5 if dk else 1.0
+    return sizes, (pq, sq, pk, sk, pv, sv, pd, sd, pb, sb, scale)
+
+
+def gated_delta(q, k, v, decay, beta, sequences=None, *, key_heads=None, scale=None, h0=None, last=False, carry=False, out=None):
+    """The gated delta rule along every sequence: S <- e^decay S, e = v - S^T k, S <- S + beta k e^T, o = scale S^T q for each head:
+    (o, last, carry).
+
+    q, k: (rows, key_heads x dk); v: (rows, heads x dv); decay, beta: (rows, heads), float32, any row stride.  key_heads divides heads
+    (None: the same number); scale: None = dk^-0.5.  sequences: as gated_scan's; rows of no sequence are left as they were in `out`, and
+    zeros where the call makes o.  h0: the states in front of the first rows, (n, heads, dk, dv) float32, None = zeros.  last=True: the
+    states behind the last rows, likewise, else None.  carry=True: what gated_delta_backward starts from, else None."""
+    sizes, args = _delta_inputs(q, k, v, decay, beta, key_heads, scale)
+    seq, n = _sequences(sequences, q, out is None)
+    o = _new(v) if out is None else out
+    po, so = _rows("out", o, q, shape=v.shape)
+    states = (n, sizes[2], sizes[4], sizes[5])
+    p0 = _floats("h0", h0, q, *states)
+    nc, nb, _ = _delta_sizes(*sizes, n)
+    end = torch.empty(states, dtype=torch.float32, device=q.device) if last else None
+    car = torch.empty(nc, dtype=torch.float32, device=q.device) if carry else None
+    ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
+    _call(q, "amp_gated_delta_forward", _delta_shape(*sizes), *args, ct.byref(seq), p0, po, so, _ptr(end), _ptr(car), _ptr(ws), nb)
+    if out is not None:
+        _written((out,))
+    return o, end, car
+
+
+def gated_delta_backward(do, q, k, v, decay, beta, carry, sequences=None, *, key_heads=None, scale=None, dlast=None, out=None):
+    """(dq, dk, dv, ddecay, dbeta, dh0) from the gradient of o (and of last: dlast), the inputs and the carry of
+    gated_delta(.., carry=True).  out: five tensors for all but dh0, in which rows of no sequence are left as they were; where the
+    call makes them, the gradients of those rows are zeros."""
+    sizes, args = _delta_inputs(q, k, v, decay, beta, key_heads, scale)
+    pd, sd = _rows("do", do, q, shape=v.shape)
+    seq, n = _sequences(sequences, q, out is None)
+    if out is not None and not (isinstance(out, (tuple, list)) and len(out) == 5):
+        _refuse("out is not five tensors")
+    grads = tuple(out) if out is not None else (_new(q), _new(k), _new(v), _new(decay), _new(beta))
+    to = []
+    for name, g, x in zip(("dq", "dk", "dv", "ddecay", "dbeta"), grads, (q, k, v, decay, beta)):
+        to += _rows(name, g, q, _FLOAT_ROWS if x is decay or x is beta else DTYPES, x.shape)
+    states = (n, sizes[2], sizes[4], sizes[5])
+    nc, _, nb = _delta_sizes(*sizes, n)
+    if carry is None:
+        _refuse("carry is needed")
+    pc, pl = _floats("carry", carry, q, nc), _floats("dlast", dlast, q, *states)
+    dh0 = torch.empty(states, dtype=torch.float32, device=q.device)
+    ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
+    _call(q, "amp_gated_delta_backward", _delta_shape(*sizes), pd, sd, pl, *args, ct.byref(seq), pc, *to, dh0.data_ptr(), _ptr(ws), nb)
+    if out is not None:
+        _written(grads)
+    return grads + (dh0,)
+
+
+def gated_delta_step(q, k, v, decay, beta, state, *, key_heads=None, scale=None, out=None):
+    """One row of every sequence: state (rows, heads, dk, dv; float32, contiguous but for the distance of its rows) is brought up to
+    date in place; returns o."""
+    sizes, args = _delta_inputs(q, k, v, decay, beta, key_heads, scale)
+    _, rows, heads, _, dk, dv = sizes
+    if not isinstance(state, torch.Tensor) or state.dtype != torch.float32 or state.shape != (rows, heads, dk, dv) or \
+            state.get_device() != q.get_device() or (rows > 0 and not state[0].is_contiguous()):
+        _refuse("state is not a float32 tensor of shape %s on %s whose rows are contiguous" % ((rows, heads, dk, dv), q.device))
+    if state.requires_grad and torch.is_grad_enabled():
+        _differentiated("state")
+    o = _new(v) if out is None else out
+    po, so = _rows("out", o, q, shape=v.shape)
+    _call(q, "amp_gated_delta_step", _delta_shape(*sizes), *args, state.data_ptr(), state.stride(0), po, so)
+    _written((state,) if out is None else (state, out))
+    return o
+
+
 # ------------------------------------------------------------------ distillation
 def distill_loss(logits, teacher, index, temperature=1.0, weight=None, *, grad=True, out=None):
     """(loss, dlogits): per row weight * T^2 * KL(softmax(teacher / T) || softmax(logits / T)) over the teacher's top entries (teacher:
