@@ -637,6 +637,44 @@ int amp_gated_delta_step(const amp_delta_shape *shape, const void *q, size_t q_s
                          size_t v_stride, const float *decay, size_t decay_stride, const float *beta, size_t beta_stride, float scale,
                          float *state, size_t state_stride, void *o, size_t o_stride, void *hip_stream);
 
+/* Clipped policy loss, the loss and the gradient that starts
+ * backpropagation in one call.  Row by row, with lp = log softmax(logits /
+ * temperature) at the class index (index_bytes 4 or 8), ratio r = e^(lp - old)
+ * and d = reference - lp:
+ *   loss = weight (-min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *                  + kl (e^d - d - 1)),   A = advantage
+ *   dlogits_j = weight / temperature (1[j = index] - softmax_j)
+ *               (-(A r where r is not beyond the limit on A's side) + kl (1 - e^d))
+ * A >= 0 limits r from above, A < 0 from below; at the limit itself the
+ * gradient counts.  old NULL: r = 1, the gradient that of -A lp; reference
+ * NULL: no term of d; weight NULL: 1.  A row of weight 0 has a loss and a
+ * gradient of 0, whatever its numbers, and is read for logprob only; a row
+ * whose class is outside 0 .. classes - 1 is not read, its three results are 0.
+ * loss, logprob (lp), dlogits (may be logits, same address and stride): each
+ * may be NULL; advantage is read for loss and dlogits only.
+ * temperature 1e-6 .. 1e6, 0 <= clip_low <= 1, 0 <= clip_high. */
+int amp_policy_loss(int dtype, size_t rows, size_t classes, const void *logits, size_t logits_stride, const void *index, int index_bytes,
+                    double temperature, const float *advantage, const float *old, const float *reference, double kl, double clip_low,
+                    double clip_high, const float *weight, float *loss, float *logprob, void *dlogits, size_t dlogits_stride,
+                    void *hip_stream);
+
+/* The norm of all elements of n tensors together (the root of the sum of
+ * their squares, formed in 64 bits), and the tensors times
+ * min(1, max_norm / norm): tensor i has n consecutive elements of dtype at p,
+ * its result goes to out (NULL: none; p: in place).  A norm that is not finite
+ * leaves the elements as they are, as one up to max_norm does.  norm: a float
+ * (may be NULL).  Results overlap nothing but their own tensor.  The list is
+ * read during the call. */
+typedef struct amp_tensor {
+  const void *p;
+  void *out;
+  size_t n;
+  int32_t dtype;
+} amp_tensor;
+int amp_clip_workspace(size_t n, const amp_tensor *tensors, size_t *bytes);
+int amp_clip_gradients(size_t n, const amp_tensor *tensors, double max_norm, float *norm, void *workspace, size_t workspace_bytes,
+                       void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -77,7 +77,14 @@ class DeltaShape(ct.Structure):
 
 
 _ctxp = ct.c_void_p
-_i, _n, _p, _f = ct.c_int, ct.c_size_t, ct.c_void_p, ct.c_float   # operators' arguments: int, size or stride, device pointer, float
+
+
+class Tensor(ct.Structure):
+    _fields_ = [("p", ct.c_void_p), ("out", ct.c_void_p), ("n", ct.c_size_t), ("dtype", ct.c_int32)]
+
+
+# operators' arguments: int, size or stride, device pointer, float, double
+_i, _n, _p, _f, _d = ct.c_int, ct.c_size_t, ct.c_void_p, ct.c_float, ct.c_double
 _rows5 = [_p, _n] * 5   # q, k, v, decay, beta with their strides
 SIGNATURES = {
     "amp_create": (ct.c_int, [ct.POINTER(_ctxp), ct.c_void_p, ct.c_size_t, ct.c_void_p]),
@@ -145,6 +152,9 @@ SIGNATURES = {
     "amp_gated_delta_backward": (_i, [ct.POINTER(DeltaShape), _p, _n, _p] + _rows5 + [_f, ct.POINTER(Sequences), _p] + _rows5 +
                                  [_p, _p, _n, _p]),
     "amp_gated_delta_step": (_i, [ct.POINTER(DeltaShape)] + _rows5 + [_f, _p, _n, _p, _n, _p]),
+    "amp_policy_loss": (_i, [_i, _n, _n, _p, _n, _p, _i, _d, _p, _p, _p, _d, _d, _d, _p, _p, _p, _p, _n, _p]),
+    "amp_clip_workspace": (_i, [_n, _p, ct.POINTER(_n)]),
+    "amp_clip_gradients": (_i, [_n, _p, _d, _p, _p, _n, _p]),
     "amp_distill_workspace": (_i, [_i, _n, _n, ct.POINTER(_n)]),
     "amp_distill_loss": (_i, [_i, _n, _n, _p, _n, _n, _i, _p, _n, _p, _i, _n, _f, _p, _p, _p, _n, _p, _n, _p]),
 }

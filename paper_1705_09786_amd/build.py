@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libamp.so")
 LIB_STRICT = os.path.join(HERE, "libamp_strict.so")
 SOURCES = ["amp_tree.hip", "amp_ggnn.hip", "amp_rnn.hip", "amp_mlp.hip", "amp_kernels.hip", "amp_delta.hip", "amp_scan.hip",
-           "amp_norm.hip", "amp_distill.hip", "amp_lib.cpp", "amp_ops.cpp"]
+           "amp_norm.hip", "amp_distill.hip", "amp_policy.hip", "amp_clip.hip", "amp_lib.cpp", "amp_ops.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 

@@ -1,7 +1,11 @@
 // C entry points of the operators on whole arrays (include/amp.h): argument checks and launches.  Nothing here allocates, waits or
 // throws.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
+
+#include <algorithm>
 
 #include "../../include/amp.h"
 #include "amp_ops.h"
@@ -174,6 +178,61 @@ void delta_in(DeltaArgs& a, const amp_delta_shape* s, const DeltaIn& q, const De
 
 size_t delta_carry_floats(const amp_delta_shape* s, size_t n) {
   return s->rows * s->heads * s->dv + amp_delta_blocks(s->rows, n) * s->heads * s->dk * s->dv;
+}
+
+constexpr size_t MAX_TENSORS = (size_t)1 << 20, MAX_ELEMENTS = (size_t)1 << 40;
+
+static_assert(sizeof(ClipTensor) == sizeof(amp_tensor) && offsetof(ClipTensor, dtype) == offsetof(amp_tensor, dtype), "one layout");
+
+int check_tensors(const char* what, size_t n, const amp_tensor* t) {
+  if (n > MAX_TENSORS) return fail(AMP_EINVAL, "%s: %zu tensors, up to 2^20 are taken", what, n);
+  if (n && !t) return fail(AMP_EINVAL, "%s: tensors is NULL", what);
+  size_t total = 0;
+  for (size_t i = 0; i < n; ++i) {
+    if (t[i].dtype < AMP_F32 || t[i].dtype > AMP_F16) return fail(AMP_EINVAL, "%s: tensor %zu: unknown dtype %d", what, i, t[i].dtype);
+    if (t[i].n > MAX_ELEMENTS || (total += t[i].n) > MAX_ELEMENTS) return fail(AMP_EINVAL, "%s: more than 2^40 elements", what);
+    if (!t[i].n) continue;
+    if (!t[i].p) return fail(AMP_EINVAL, "%s: tensor %zu is NULL", what, i);
+    if (((uintptr_t)t[i].p | (uintptr_t)t[i].out) % elem(t[i].dtype))
+      return fail(AMP_EINVAL, "%s: tensor %zu is not aligned to its elements", what, i);
+  }
+  return AMP_OK;
+}
+
+// Memory that a tensor is read from, or its result written to.
+struct Range {
+  uintptr_t first, last;
+  size_t tensor;   // -1: the norm or the workspace
+  bool written;
+};
+
+// No result overlaps anything but its own tensor, and that only as a whole.
+int check_results(const char* what, size_t n, const amp_tensor* t, const float* norm, const void* ws, size_t need) {
+  Range* r = (Range*)malloc((2 * n + 2) * sizeof(Range));
+  if (!r) return fail(AMP_ENOMEM, "%s: no host memory for %zu ranges", what, 2 * n + 2);
+  size_t m = 0;
+  for (size_t i = 0; i < n; ++i) {
+    if (!t[i].n) continue;
+    const size_t bytes = t[i].n * elem(t[i].dtype);
+    r[m++] = {(uintptr_t)t[i].p, (uintptr_t)t[i].p + bytes, i, t[i].p == t[i].out};
+    if (t[i].out && t[i].out != t[i].p) r[m++] = {(uintptr_t)t[i].out, (uintptr_t)t[i].out + bytes, i, true};
+  }
+  if (norm) r[m++] = {(uintptr_t)norm, (uintptr_t)norm + sizeof(float), (size_t)-1, true};
+  if (need) r[m++] = {(uintptr_t)ws, (uintptr_t)ws + need, (size_t)-1, true};
+  std::sort(r, r + m, [](const Range& a, const Range& b) { return a.first < b.first; });
+  // in the order of their beginnings, a range meets one in front of it where that, or one further in front, ends behind its beginning
+  uintptr_t any = 0, written = 0;
+  size_t bad = m;
+  for (size_t i = 0; i < m && bad == m; ++i) {
+    if (r[i].first < written || (r[i].written && r[i].first < any)) bad = i;
+    any = std::max(any, r[i].last);
+    if (r[i].written) written = std::max(written, r[i].last);
+  }
+  const size_t tensor = bad < m ? r[bad].tensor : 0;
+  free(r);
+  if (bad == m) return AMP_OK;
+  if (tensor == (size_t)-1) return fail(AMP_EINVAL, "%s: norm or workspace overlaps a tensor or a result", what);
+  return fail(AMP_EINVAL, "%s: tensor %zu overlaps a result, or its result another tensor", what, tensor);
 }
 
 }  // namespace
@@ -512,6 +571,59 @@ int amp_distill_loss(int dtype, size_t rows, size_t classes, const void* logits,
   a.teacher_stride = teacher_stride, a.index_stride = index_stride, a.temperature = temperature, a.weight = weight;
   a.loss = loss, a.dlogits = dlogits, a.dlogits_stride = dlogits_stride, a.workspace = workspace;
   return launched(what, amp_distill_launch(dtype, &a, (hipStream_t)hip_stream));
+}
+
+int amp_policy_loss(int dtype, size_t rows, size_t classes, const void* logits, size_t logits_stride, const void* index, int index_bytes,
+                    double temperature, const float* advantage, const float* old, const float* reference, double kl, double clip_low,
+                    double clip_high, const float* weight, float* loss, float* logprob, void* dlogits, size_t dlogits_stride,
+                    void* hip_stream) {
+  const char* what = "policy_loss";
+  CHECK(check_size(what, dtype, rows, classes, "classes"));
+  if (index_bytes != 4 && index_bytes != 8) return fail(AMP_EINVAL, "%s: index_bytes %d, 4 and 8 are taken", what, index_bytes);
+  if (!(temperature >= 1e-6 && temperature <= 1e6)) return fail(AMP_EINVAL, "%s: temperature %g, 1e-6 .. 1e6 are taken", what, temperature);
+  if (!(clip_low >= 0.0 && clip_low <= 1.0)) return fail(AMP_EINVAL, "%s: clip_low %g, 0 .. 1 are taken", what, clip_low);
+  if (!(clip_high >= 0.0)) return fail(AMP_EINVAL, "%s: clip_high %g, 0 and more are taken", what, clip_high);
+  if (!(fabs(kl) < INFINITY)) return fail(AMP_EINVAL, "%s: kl %g is not finite", what, kl);
+  if (rows == 0 || (!loss && !logprob && !dlogits)) return AMP_OK;
+  REQUIRE(logits);
+  REQUIRE(index);
+  if (loss || dlogits) REQUIRE(advantage);
+  const size_t e = elem(dtype);
+  const Span s[] = {{"dlogits", dlogits, rows, classes, dlogits_stride, e}, {"loss", loss, 1, rows, rows, 4},
+                    {"logprob", logprob, 1, rows, rows, 4},                 {"logits", logits, rows, classes, logits_stride, e},
+                    {"index", index, 1, rows, rows, (size_t)index_bytes},   {"advantage", advantage, 1, rows, rows, 4},
+                    {"old", old, 1, rows, rows, 4},                         {"reference", reference, 1, rows, rows, 4},
+                    {"weight", weight, 1, rows, rows, 4}};
+  CHECK(check_arrays(what, s, 3));
+  const int pair[][2] = {{0, 3}};
+  CHECK(check_overlaps(what, s, 3, pair, 1));
+  PolicyArgs a = {};
+  a.rows = rows, a.classes = classes, a.logits = logits, a.logits_stride = logits_stride, a.index = index, a.index_bytes = index_bytes;
+  a.inverse = 1.0 / temperature, a.scale = 1.4426950408889634074 / temperature;
+  a.kl = kl, a.low = 1.0 - clip_low, a.high = 1.0 + clip_high, a.log_low = log1p(-clip_low), a.log_high = log1p(clip_high);
+  a.advantage = advantage, a.old = old, a.reference = reference, a.weight = weight;
+  a.loss = loss, a.logprob = logprob, a.dlogits = dlogits, a.dlogits_stride = dlogits_stride;
+  return launched(what, amp_policy_launch(dtype, &a, (hipStream_t)hip_stream));
+}
+
+int amp_clip_workspace(size_t n, const amp_tensor* tensors, size_t* bytes) {
+  const char* what = "clip_workspace";
+  CHECK(check_tensors(what, n, tensors));
+  REQUIRE(bytes);
+  *bytes = amp_clip_workspace_bytes(n, (const ClipTensor*)tensors);
+  return AMP_OK;
+}
+
+int amp_clip_gradients(size_t n, const amp_tensor* tensors, double max_norm, float* norm, void* workspace, size_t workspace_bytes,
+                       void* hip_stream) {
+  const char* what = "clip_gradients";
+  CHECK(check_tensors(what, n, tensors));
+  if (!(max_norm >= 0.0)) return fail(AMP_EINVAL, "%s: max_norm is negative or not a number", what);
+  if ((uintptr_t)norm % sizeof(float)) return fail(AMP_EINVAL, "%s: norm is not aligned to its 4-byte elements", what);
+  const size_t need = amp_clip_workspace_bytes(n, (const ClipTensor*)tensors);
+  CHECK(check_workspace(what, workspace, workspace_bytes, need));
+  CHECK(check_results(what, n, tensors, norm, workspace, need));
+  return launched(what, amp_clip_launch(n, (const ClipTensor*)tensors, max_norm, norm, workspace, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

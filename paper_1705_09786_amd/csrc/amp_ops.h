@@ -106,6 +106,37 @@ struct DeltaStepArgs {
   size_t o_stride;
 };
 
+struct PolicyArgs {
+  size_t rows, classes, row0;   // row0: a launch's first row
+  const void* logits;
+  size_t logits_stride;
+  const void* index;
+  int index_bytes;
+  double inverse, scale;                     // 1 and log2(e) over the temperature
+  double kl, low, high, log_low, log_high;   // the ratio's limits
+  const float *advantage, *old, *reference, *weight;
+  float *loss, *logprob;
+  void* dlogits;
+  size_t dlogits_stride;
+};
+
+struct ClipTensor {
+  const void* p;
+  void* out;
+  size_t n;
+  int dtype;
+};
+
+#define CLIP_LIST 140   // tensors of a launch, whose arguments are at most 4 KB
+struct ClipList {
+  const void* p[CLIP_LIST];
+  void* out[CLIP_LIST];
+  size_t count[CLIP_LIST];   // elements << 2 | dtype
+  unsigned first[CLIP_LIST + 1];
+  int n;
+  size_t piece;
+};
+
 extern "C" {
 size_t amp_norm_workspace_bytes(int dtype, size_t rows, size_t cols);
 hipError_t amp_norm_forward_launch(int dtype, const NormArgs* a, hipStream_t stream);
@@ -120,6 +151,9 @@ size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t dk,
 hipError_t amp_delta_forward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
 hipError_t amp_delta_backward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
 hipError_t amp_delta_step_launch(int dtype, const DeltaStepArgs* a, hipStream_t stream);
+hipError_t amp_policy_launch(int dtype, const PolicyArgs* a, hipStream_t stream);
+size_t amp_clip_workspace_bytes(size_t n, const ClipTensor* t);
+hipError_t amp_clip_launch(size_t n, const ClipTensor* t, double max_norm, float* norm, void* workspace, hipStream_t stream);
 size_t amp_distill_workspace_bytes(int dtype, size_t rows, size_t classes);
 hipError_t amp_distill_launch(int dtype, const DistillArgs* a, hipStream_t stream);
 }

@@ -11,6 +11,7 @@ backward of a torch.autograd.Function); writes to a caller's tensor count as in-
 from __future__ import annotations
 
 import ctypes as ct
+from array import array
 from functools import lru_cache
 
 import torch
@@ -394,3 +395,92 @@ def distill_loss(logits, teacher, index, temperature=1.0, weight=None, *, grad=T
     if out is not None:
         _written((out,))
     return loss, dlogits
+
+
+# ------------------------------------------------------------------ policy loss
+def _classes(index, like, rows):
+    """A class a row: (address, bytes of an element)."""
+    if not isinstance(index, torch.Tensor) or index.dtype not in _INDEX or index.shape != (rows,) or not index.is_contiguous() or \
+            index.get_device() != like.get_device():
+        _refuse("index is not a contiguous int32 or int64 tensor of shape %s on %s" % ((rows,), like.device))
+    return index.data_ptr(), _INDEX[index.dtype]
+
+
+def policy_loss(logits, index, old, advantage, *, reference=None, kl=0.0, clip=0.2, temperature=1.0, weight=None, grad=True, out=None):
+    """(loss, logprob, dlogits): per row, with lp = log softmax(logits / temperature)[index], r = e^(lp - old) and d = reference - lp,
+    weight * (-min(r A, clamp(r, 1 - clip, 1 + clip) A) + kl (e^d - d - 1)), A the advantage; lp; and the gradient of the losses' sum
+    by the logits, in their type (None without grad).  index: int32 or int64 (rows); old (None: r = 1, the gradient that of -A lp), advantage,
+    reference (None: no term of d), weight (None: 1): a float per row.  clip: a number, or the pair (below, above).  Rows of weight 0
+    have no loss and no gradient, rows whose index is no class zeros in all three.  out: a tensor for dlogits (may be logits)."""
+    px, sx = _rows("logits", logits)
+    rows, classes = shape = logits.shape
+    pi, size = _classes(index, logits, rows)
+    if advantage is None:
+        _refuse("advantage is needed")
+    pa, po = _floats("advantage", advantage, logits, rows), _floats("old", old, logits, rows)
+    pr, pw = _floats("reference", reference, logits, rows), _floats("weight", weight, logits, rows)
+    if isinstance(clip, (tuple, list)):
+        if len(clip) != 2:
+            _refuse("clip is not a number or a pair of numbers")
+        low, high = clip
+    else:
+        low = high = clip
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    logprob = torch.empty_like(loss)
+    dlogits, pd, sd = None, None, 0
+    if grad:
+        dlogits = _new(logits) if out is None else out
+        pd, sd = _rows("out", dlogits, logits, shape=shape)
+    elif out is not None:
+        _refuse("out without grad")
+    _call(logits, "amp_policy_loss", DTYPES[logits.dtype], rows, classes, px, sx, pi, size, temperature, pa, po, pr, kl, low, high, pw,
+          loss.data_ptr(), logprob.data_ptr(), pd, sd)
+    if out is not None:
+        _written((out,))
+    return loss, logprob, dlogits
+
+
+def token_logprob(logits, index, temperature=1.0):
+    """log softmax(logits / temperature)[index] of every row, float32: what policy_loss takes for old and reference; 0 where index is no
+    class."""
+    px, sx = _rows("logits", logits)
+    rows, classes = logits.shape
+    pi, size = _classes(index, logits, rows)
+    logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    _call(logits, "amp_policy_loss", DTYPES[logits.dtype], rows, classes, px, sx, pi, size, temperature, None, None, None, 0.0, 0.0, 0.0, None,
+          None, logprob.data_ptr(), None, 0)
+    return logprob
+
+
+# ------------------------------------------------------------------ norm and clipping
+def clip_gradients(gradients, max_norm=None, *, out=None):
+    """The norm of all elements of the tensors together, a float32 tensor without dimensions; with max_norm the tensors are multiplied by
+    min(1, max_norm / norm), in place or into the tensors of `out` (of the same shapes and types).  gradients: contiguous tensors of any
+    shapes on one GPU, float32, bfloat16 or float16.  A norm that is not finite leaves them as they are."""
+    gradients = list(gradients)
+    if not gradients:
+        _refuse("there are no gradients")
+    if out is not None and max_norm is None:
+        _refuse("out without max_norm")
+    results = None if max_norm is None else gradients if out is None else list(out)
+    first = gradients[0]
+    grad_mode, device = torch.is_grad_enabled(), first.get_device() if isinstance(first, torch.Tensor) else -1
+    for name, tensors in (("gradients", gradients),) + ((("out", results),) if out is not None else ()):
+        for i, t in enumerate(tensors):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in DTYPES or t.get_device() != device or not t.is_contiguous():
+                _refuse("%s[%d] is not a contiguous tensor of a float type on the GPU of the first" % (name, i))
+            if grad_mode and t.requires_grad:
+                _differentiated("%s[%d]" % (name, i))
+    if out is not None and ([t.shape for t in results] != [t.shape for t in gradients] or [t.dtype for t in results] != [t.dtype for t in gradients]):
+        _refuse("out has other shapes or types than the gradients")
+    p = [t.data_ptr() for t in gradients]
+    to = [0] * len(p) if results is None else p if out is None else [t.data_ptr() for t in results]
+    table = array("Q", [x for item in zip(p, to, [t.numel() for t in gradients], [DTYPES[t.dtype] for t in gradients]) for x in item])
+    at, nb = table.buffer_info()[0], ct.c_size_t()
+    _check(B.lib().amp_clip_workspace(len(p), at, ct.byref(nb)))
+    norm = torch.empty((), dtype=torch.float32, device=first.device)
+    ws = torch.empty(nb.value, dtype=torch.uint8, device=first.device)
+    _call(first, "amp_clip_gradients", len(p), at, float("inf") if max_norm is None else max_norm, norm.data_ptr(), ws.data_ptr(), nb.value)
+    if results is not None:
+        _written(tuple(results))
+    return norm
