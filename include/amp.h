@@ -601,8 +601,9 @@ int amp_distill_loss(int dtype, size_t rows, size_t classes, const void *logits,
  * 0 .. 2 and decays of at most 0 (-infinity forgets the state), where errors
  * do not grow; other values are taken as the formula has them.  A value that
  * is not finite may reach every row of its sequence and head, none of others.
- * dk 1 .. 128, dv 1 .. 1024, heads below 2^16, fewer than 2^30 rows; at most
- * 2^22 of (rows / 64 + sequences) x heads.
+ * dk 1 .. 128, dv 1 .. 1024, heads below 2^16, rows of fewer than 2^22
+ * elements, strides of q, k, v, o and dout below 2^22 (but in a step), fewer
+ * than 2^30 rows; at most 2^22 of (rows / 64 + sequences) x heads.
  *
  * h0 (may be NULL = zeros): states in front of the first rows.  last (may be
  * NULL): states behind the last rows, h0 for an empty sequence.  carry (may be

@@ -44,12 +44,17 @@ struct Frag {
 
 template <int P>
 __device__ __forceinline__ void split2(float a, float b, unsigned (&u)[P]) {
+  // what a part leaves of its number, exactly, in one instruction: a - 1 u.lo - 0 u.hi. (The factors pass through registers: as a
+  // constant -1 the instruction would take the upper half.)
+  unsigned lo = 0xbf80u, hi = 0xbf800000u;
+  asm("" : "+s"(lo));
+  asm("" : "+s"(hi));
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     u[i] = pack2(a, b, bf16());
     if (i + 1 < P) {
-      a -= __uint_as_float(u[i] << 16);
-      b -= __uint_as_float(u[i] & 0xffff0000u);
+      a = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i]), __builtin_bit_cast(v2bf, lo), a, false);
+      b = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i]), __builtin_bit_cast(v2bf, hi), b, false);
     }
   }
 }
@@ -163,39 +168,108 @@ __device__ __forceinline__ bool find_block(const DeltaArgs& a, size_t index, Blo
   return w.count > 0;
 }
 
-// N and P of a chunk, the sums of decays of a block's two chunks (in 64 bits: differences of far sums decide about near rows).
+// N and P of a chunk; e^G, e^{G_end - G} and beta of a block's rows and e^{G_end} of its two chunks; the sums G of decays (in 64 bits:
+// differences of far sums decide about near rows).
 __device__ __forceinline__ float* matrices_of(const DeltaArgs& a, size_t block, int h, int chunk) {
   return a.matrices + ((block * a.heads + h) * 2 + chunk) * (2 * C * C);
 }
+__device__ __forceinline__ float* scalars_of(const DeltaArgs& a, size_t block, int h) { return a.scalars + (block * a.heads + h) * (4 * B); }
 __device__ __forceinline__ double* sums_of(const DeltaArgs& a, size_t block, int h) { return a.sums + (block * a.heads + h) * B; }
 __device__ __forceinline__ size_t state_at(const DeltaArgs& a, size_t index, int h) { return (index * a.heads + h) * ((size_t)a.dk * a.dv); }
 
 // ------------------------------------------------------------------ plan
+// A long sequence is cut into segments whose chains run side by side, where that is sooner: every segment but its last passes once more
+// without outputs, for the map from the state in front of it to the one behind it (dk columns beside the dv), and a short chain over the
+// segments joins those. `longest` and `all` blocks, `work` workgroups to a block's chain: the chain alone takes the longest sequence's blocks,
+// or all of them over the compute units; with segments two and a half times the latter and some blocks' time for the join. Blocks of
+// a segment; 1 << 30: whole sequences.
+__host__ __device__ inline long segment_blocks(long longest, long all, long work) {
+  const long share = (all * work + 255) / 256;
+  if (longest < 24 || longest <= share * 5 / 2 + 8) return (long)1 << 30;
+  long root = DELTA_SEGMENT;   // a segment's blocks pass twice, and are a step of the join
+  while (root * root * 4 < longest) ++root;
+  return root > share ? root : share;
+}
+
+struct Job {
+  size_t s;          // its sequence
+  long from, to;     // its blocks, counted in the sequence
+  bool first, last;  // of the sequence's segments
+};
+// Segment `index` of all of them.
+__device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& w) {
+  if (!a.segments) {
+    w.s = index, w.from = 0, w.to = first_block(a, index + 1) - first_block(a, index), w.first = w.last = true;
+    return index < a.n_seq;
+  }
+  size_t lo = 0, hi = a.n_seq;
+  long size = a.segment;
+  if (a.begin) {
+    size = a.first_segment[a.n_seq + 1];
+    if ((long)index >= a.first_segment[hi]) return false;
+    while (hi - lo > 1) {
+      const size_t mid = (lo + hi) / 2;
+      (a.first_segment[mid] <= (long)index ? lo : hi) = mid;
+    }
+    index -= a.first_segment[lo];
+  }
+  const long blocks = first_block(a, lo + 1) - first_block(a, lo), count = blocks > size ? (blocks + size - 1) / size : 1;
+  if ((long)index >= count) return false;
+  w.s = lo, w.from = (long)index * size, w.to = w.from + size < blocks ? w.from + size : blocks;
+  w.first = index == 0, w.last = (long)index + 1 == count;
+  return true;
+}
+__device__ __forceinline__ size_t first_segment(const DeltaArgs& a, size_t s) { return a.begin ? a.first_segment[s] : 0; }
+
 constexpr int PLAN = 1024;
-__global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a) {
+// Sums in front of every thread's value; `base` goes on by the sum of all.
+__device__ __forceinline__ long sum_in_front(long mine, long& base, long (&part)[PLAN / 64]) {
+  long sum = mine;
+  for (int d = 1; d < 64; d *= 2) {
+    const long up = __shfl_up(sum, d, 64);
+    if ((int)(threadIdx.x & 63) >= d) sum += up;
+  }
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  long front = base + sum - mine;
+  for (int w = 0; w < PLAN / 64; ++w) {
+    if (w < (int)(threadIdx.x >> 6)) front += part[w];
+    base += part[w];
+  }
+  __syncthreads();
+  return front;
+}
+
+__global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work) {
   __shared__ long part[PLAN / 64];
-  long base = 0;
+  const long most = (long)a.blocks;
+  long base = 0, longest = 0;
   for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
     const size_t s = s0 + threadIdx.x;
     long b = 0, e = 0;
     if (s < a.n_seq) span(a, s, b, e);
-    const long mine = (e - b + B - 1) / B;
-    long sum = mine;
-    for (int d = 1; d < 64; d *= 2) {
-      const long up = __shfl_up(sum, d, 64);
-      if ((int)(threadIdx.x & 63) >= d) sum += up;
-    }
-    if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    long front = base;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) front += part[w];
-    const long at = front + sum - mine;
-    if (s < a.n_seq) a.first[s] = at < (long)a.blocks ? (int)at : (int)a.blocks;
-    for (int w = threadIdx.x >> 6; w < PLAN / 64; ++w) front += part[w];
-    base = front;
-    __syncthreads();
+    const long mine = (e - b + B - 1) / B, at = sum_in_front(mine, base, part);
+    longest = mine > longest ? mine : longest;
+    if (s < a.n_seq) a.first[s] = (int)(at < most ? at : most);
   }
-  if (threadIdx.x == 0) a.first[a.n_seq] = base < (long)a.blocks ? (int)base : (int)a.blocks;
+  const long all = base < most ? base : most;
+  if (threadIdx.x == 0) a.first[a.n_seq] = (int)all;
+  if (!a.segments) return;
+  for (int d = 1; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d, 64));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = longest;
+  __syncthreads();
+  for (int w = 0; w < PLAN / 64; ++w) longest = max(longest, part[w]);
+  __syncthreads();
+  const long size = segment_blocks(longest < all ? longest : all, all, work);
+  base = 0;
+  for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
+    const size_t s = s0 + threadIdx.x;
+    long blocks = 0;
+    if (s < a.n_seq) blocks = a.first[s + 1] - a.first[s];   // written by this workgroup, a barrier ago
+    const long count = s < a.n_seq ? (blocks > size ? (blocks + size - 1) / size : 1) : 0, at = sum_in_front(count, base, part);
+    if (s < a.n_seq) a.first_segment[s] = (int)at;
+  }
+  if (threadIdx.x == 0) a.first_segment[a.n_seq] = (int)base, a.first_segment[a.n_seq + 1] = (int)size;
 }
 
 // Rows of no sequence: a wave to a row, zeros in every output.
@@ -262,6 +336,12 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
     g[lane] = sum;
     beta[lane] = bt;
     sums_of(a, w.index, h)[lane] = sum;
+    const double end = __shfl(sum, C - 1, C);
+    float* f = scalars_of(a, w.index, h);
+    f[lane] = expf((float)sum);
+    f[B + lane] = expf((float)(end - sum));
+    f[2 * B + lane] = bt;
+    if (lane % C == 0) f[3 * B + lane / C] = expf((float)end);
   }
   __syncthreads();
   {   // a wave to each product of each chunk: its three tiles that have elements on or below the diagonal
@@ -309,84 +389,112 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
 }
 
 // ------------------------------------------------------------------ the chain over a sequence's chunks
-// What a chunk's waves share, on its way from memory and in LDS.
-template <class T, int KT, int W, int PN>
+// base + bytes, for a base that is the same for all lanes.
+template <class T>
+__device__ __forceinline__ const T* past(const T* base, unsigned bytes) { return (const T*)((const char*)base + bytes); }
+template <class T>
+__device__ __forceinline__ T* past(T* base, unsigned bytes) { return (T*)((char*)base + bytes); }
+
+// What a chunk's waves share, on its way from memory and in LDS. OUT: with Q and P (in PN parts), else K and N alone.
+template <class T, int KT, int W, int PN, bool OUT>
 struct Chunk {
-  static constexpr int P = In<T>::P, LD = KT * 32 + 8, UNITS = C * KT * 8, PER = (UNITS + 64 * W - 1) / (64 * W), PAIR = 2 * C * C / 4 / (64 * W);
+  static constexpr int P = In<T>::P, LD = KT * 32 + 8, UNITS = C * KT * 8, STEP = 64 * W / (KT * 8), PER = (UNITS + 64 * W - 1) / (64 * W);
+  static constexpr int FOURS = (OUT ? 2 : 1) * C * C / 4, PAIR = (FOURS + 64 * W - 1) / (64 * W);
   struct Shared {
-    Matrix<P, C, LD> k, q;
+    Matrix<P, C, LD> k;
+    Matrix<OUT ? P : 1, OUT ? C : 1, OUT ? LD : 8> q;
     Matrix<3, C, C + 8> n;
-    Matrix<PN, C, C + 8> p;
-    float beta[C], grow[C], rest[C], whole;
+    Matrix<PN, OUT ? C : 1, C + 8> p;
+    alignas(16) float grow[C], rest[C], beta[C], whole;
   };
-  Vec<T, 4> k[PER], q[PER];
+  Vec<T, 4> k[PER], q[OUT ? PER : 1];
   Vec<float, 4> pair[PAIR];
-  double g, end;
-  float beta;
+  float scalar;
+  // this thread's first element of K and Q, in bytes from a chunk's, and how many of four there are; the others are STEP rows apart
+  unsigned k0, q0;
+  int n;
+  __device__ __forceinline__ explicit Chunk(const DeltaArgs& a) {
+    const int four = threadIdx.x % (KT * 8), row = threadIdx.x / (KT * 8), left = a.dk - 4 * four;
+    n = UNITS < 64 * W && (int)threadIdx.x >= UNITS ? 0 : left < 0 ? 0 : left > 4 ? 4 : left;
+    const unsigned col = n ? 4 * four : 0, r = n ? row : 0;
+    k0 = (r * (unsigned)a.k_stride + col) * (unsigned)sizeof(T);
+    q0 = (r * (unsigned)a.q_stride + col) * (unsigned)sizeof(T);
+  }
   __device__ __forceinline__ void fetch(const DeltaArgs& a, long row, int count, size_t block, int half, int h, int hk) {
     const T* K = row_of((const T*)a.k, row, a.k_stride) + (size_t)hk * a.dk;
     const T* Q = row_of((const T*)a.q, row, a.q_stride) + (size_t)hk * a.dk;
+    const int mine = threadIdx.x / (KT * 8);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const int u = threadIdx.x + j * 64 * W, r = u / (KT * 8), four = u % (KT * 8);
-      const long n = r < count ? a.dk - four * 4 : 0;
-      const int rr = r < count ? r : 0, cc = n > 0 ? four * 4 : 0;
-      k[j] = load_group<4>(K + rr * a.k_stride + cc, n);
-      q[j] = load_group<4>(Q + rr * a.q_stride + cc, n);
+      const bool in = count == C || mine + j * STEP < count;   // rows behind the sequence's end are zeros
+      k[j] = load_group<4>(past(K + (in ? j * STEP * a.k_stride : 0), in ? k0 : 0u), in ? n : 0);
+      if (OUT) q[j] = load_group<4>(past(Q + (in ? j * STEP * a.q_stride : 0), in ? q0 : 0u), in ? n : 0);
     }
     const float* m = matrices_of(a, block, h, half);
 #pragma unroll
-    for (int j = 0; j < PAIR; ++j) pair[j] = load_vec(m + (threadIdx.x + j * 64 * W) * 4, 4);
-    const double* sums = sums_of(a, block, h) + half * C;
-    g = sums[threadIdx.x % C], end = sums[C - 1];
-    const int r = threadIdx.x % C;
-    beta = r < count ? a.beta[(row + r) * a.beta_stride + h] : 0.f;
+    for (int j = 0; j < PAIR; ++j)
+      if (FOURS >= 64 * W || (int)threadIdx.x < FOURS) pair[j] = load_vec(past(m + j * 64 * W * 4, threadIdx.x * 16u), 4);
+    const float* f = scalars_of(a, block, h);
+    const int t = threadIdx.x < 3 * C ? threadIdx.x / C * B + half * C + threadIdx.x % C : 3 * B + half;
+    if (threadIdx.x <= 3 * C) scalar = f[t];
   }
   __device__ __forceinline__ void put(Shared& s) const {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const int u = threadIdx.x + j * 64 * W;
-      if (UNITS % (64 * W) && u >= UNITS) continue;
+      if (UNITS < 64 * W && (int)threadIdx.x >= UNITS) continue;
+      const int row = threadIdx.x / (KT * 8) + j * STEP, four = threadIdx.x % (KT * 8);
       v2u x[P];
       parts4(k[j], x);
-      s.k.put(u / (KT * 8), u % (KT * 8), x);
-      parts4(q[j], x);
-      s.q.put(u / (KT * 8), u % (KT * 8), x);
+      s.k.put(row, four, x);
+      if constexpr (OUT) {
+        parts4(q[j], x);
+        s.q.put(row, four, x);
+      }
     }
 #pragma unroll
     for (int j = 0; j < PAIR; ++j) {
       const int u = threadIdx.x + j * 64 * W, r = u % (C * C / 4) / (C / 4), four = u % (C / 4);
+      if (FOURS < 64 * W && u >= FOURS) continue;
       const float x[4] = {get(pair[j], 0), get(pair[j], 1), get(pair[j], 2), get(pair[j], 3)};
       if (u < C * C / 4) {
         v2u y[3];
         split4<3>(x, y);
         s.n.put(r, four, y);
-      } else {
+      } else if constexpr (OUT) {
         v2u y[PN];
         split4<PN>(x, y);
         s.p.put(r, four, y);
       }
     }
-    if (threadIdx.x < C) {
-      s.beta[threadIdx.x] = beta;
-      s.grow[threadIdx.x] = expf((float)g);
-      s.rest[threadIdx.x] = expf((float)(end - g));
-      if (threadIdx.x == 0) s.whole = expf((float)end);
-    }
+    if (threadIdx.x <= 3 * C) s.grow[threadIdx.x] = scalar;   // and rest, beta and whole behind it
   }
 };
 
 // Eight of a wave's values in a chunk: rows 4 (lane / 16) + i of its two tiles, column lane % 16 of the wave's.
 __device__ __forceinline__ int chunk_row(int k) { return (k / 4) * 16 + 4 * (threadIdx.x % 64 / 16) + k % 4; }
+struct Eight {
+  v4f t[2];
+  __device__ __forceinline__ explicit Eight(const float (&rows)[C]) {
+    t[0] = *(const v4f*)&rows[4 * (threadIdx.x % 64 / 16)];
+    t[1] = *(const v4f*)&rows[16 + 4 * (threadIdx.x % 64 / 16)];
+  }
+  __device__ __forceinline__ float operator[](int k) const { return t[k / 4][k % 4]; }
+};
 
 template <class T>
 struct Rows8 {
   T v[8];
-  __device__ __forceinline__ void fetch(const T* p, size_t stride, int count, bool column) {
+  // `lane`: bytes of row 4 (lane / 16) and the lane's column from p. Rows behind the last are read as the last: what they meet is 0.
+  __device__ __forceinline__ void fetch(const T* p, size_t stride, unsigned lane, unsigned column, int count) {
+    if (count == C) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      v[k] = (T)0.f;
-      if (column && chunk_row(k) < count) v[k] = p[chunk_row(k) * stride];
+      for (int k = 0; k < 8; ++k) v[k] = *past(p + ((k / 4) * 16 + k % 4) * stride, lane);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = chunk_row(k) < count ? chunk_row(k) : count - 1;
+        v[k] = *past(p, ((unsigned)r * (unsigned)stride + column) * (unsigned)sizeof(T));
+      }
     }
   }
 };
@@ -395,20 +503,28 @@ struct Rows8 {
 template <int KT>
 struct State {
   v4f t[2 * KT];
-  __device__ __forceinline__ void load(const DeltaArgs& a, const float* p, int col) {
+  __device__ __forceinline__ void load(const float* p, int dk, int width, int col) {
     const int r0 = 4 * (threadIdx.x % 64 / 16);
 #pragma unroll
     for (int m = 0; m < 2 * KT; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) t[m][i] = p && col < a.dv && 16 * m + r0 + i < a.dk ? p[(size_t)(16 * m + r0 + i) * a.dv + col] : 0.f;
+      for (int i = 0; i < 4; ++i) t[m][i] = p && col < width && 16 * m + r0 + i < dk ? p[(size_t)(16 * m + r0 + i) * width + col] : 0.f;
   }
-  __device__ __forceinline__ void store(const DeltaArgs& a, float* p, int col) const {
+  __device__ __forceinline__ void store(float* p, int dk, int width, int col) const {
     const int r0 = 4 * (threadIdx.x % 64 / 16);
+    if (col >= width) return;
 #pragma unroll
     for (int m = 0; m < 2 * KT; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (col < a.dv && 16 * m + r0 + i < a.dk) p[(size_t)(16 * m + r0 + i) * a.dv + col] = t[m][i];
+        if (dk == 32 * KT || 16 * m + r0 + i < dk) *past(p + (16 * m + i) * width, (unsigned)(r0 * width + col) * 4u) = t[m][i];
+  }
+  __device__ __forceinline__ void identity(int col) {
+    const int r0 = 4 * (threadIdx.x % 64 / 16);
+#pragma unroll
+    for (int m = 0; m < 2 * KT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[m][i] = 16 * m + r0 + i == col ? 1.f : 0.f;
   }
   __device__ __forceinline__ Frag<3> operand(int f) const {
     const float x[8] = {t[2 * f][0], t[2 * f][1], t[2 * f][2], t[2 * f][3], t[2 * f + 1][0], t[2 * f + 1][1], t[2 * f + 1][2], t[2 * f + 1][3]};
@@ -416,29 +532,56 @@ struct State {
   }
 };
 
-template <class T, int KT, int W>
+// What a wave of a chain works on: 16 columns of the state, or of the map that a segment is.
+struct Columns {
+  int c0, col;     // the first, the lane's
+  bool map, any;   // of the map; there are columns
+  __device__ __forceinline__ Columns(const DeltaArgs& a, int w, bool maps) {
+    const int tile = blockIdx.y * w + threadIdx.x / 64, values = (a.dv + 15) / 16;
+    map = maps && tile >= values;
+    c0 = 16 * (map ? tile - values : tile);
+    col = c0 + threadIdx.x % 16;
+    any = c0 < (map ? a.dk : a.dv);
+  }
+};
+
+__device__ __forceinline__ float* front_of(const DeltaArgs& a, size_t segment, int h) { return a.fronts + state_at(a, segment, h); }
+__device__ __forceinline__ float* map_of(const DeltaArgs& a, size_t segment, int h) {
+  return a.maps + (segment * a.heads + h) * ((size_t)a.dk * a.dk);
+}
+
+// OUT: the chain with its outputs, from the states in front of the segments; else the segments' maps, and what they leave of no state.
+template <class T, int KT, int W, bool OUT>
 __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
   constexpr int PO = sizeof(T) == 2 ? 2 : 3;   // o is rounded to 16 bits: two parts leave 2^-16 of its terms
-  typedef Chunk<T, KT, W, PO> Ck;
+  typedef Chunk<T, KT, W, PO, OUT> Ck;
   __shared__ typename Ck::Shared sh[2];
   const int h = blockIdx.x % a.heads, hk = h / (a.heads / a.key_heads);
-  const size_t s = blockIdx.x / a.heads;
-  const int lane = threadIdx.x % 64, c16 = lane % 16, q = lane / 16, c0 = (blockIdx.y * W + threadIdx.x / 64) * 16, col = c0 + c16;
+  const size_t segment = blockIdx.x / a.heads;
+  const int lane = threadIdx.x % 64, c16 = lane % 16, q = lane / 16;
+  Job w;
+  if (!find_job(a, segment, w) || (!OUT && w.last)) return;
+  const Columns m(a, W, !OUT && !w.first);
+  const int col = m.col;
   long b, e;
-  span(a, s, b, e);
-  const long first = first_block(a, s), all = first_block(a, s + 1);
-  if (e > b + (all - first) * B) e = b + (all - first) * B;
+  span(a, w.s, b, e);
+  const long first = first_block(a, w.s) + w.from;
+  b += w.from * B;
+  if (e > b + (w.to - w.from) * B) e = b + (w.to - w.from) * B;
   State<KT> S;
-  S.load(a, a.h0 ? a.h0 + state_at(a, s, h) : nullptr, col);
-  const T* V = (const T*)a.v + (size_t)h * a.dv + col;
+  if (w.first) S.load(a.h0 ? a.h0 + state_at(a, w.s, h) : nullptr, a.dk, a.dv, col);
+  else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
+  else S.identity(m.map ? col : -1);
+  const T* V = (const T*)a.v + (size_t)h * a.dv;
+  const unsigned vcol = m.map || col >= a.dv ? 0 : col, vlane = (4u * q * (unsigned)a.v_stride + vcol) * (unsigned)sizeof(T);
   const int chunks = (int)((e - b + C - 1) / C);
   const auto rows_in = [&](int c) { return e - b - (long)c * C < C ? (int)(e - b - (long)c * C) : C; };
-  Ck next;
+  Ck next(a);
   Rows8<T> vnext;
   const auto fetch = [&](int c) {
     const long row = b + (long)c * C;
     next.fetch(a, row, rows_in(c), (size_t)(first + c / 2), c % 2, h, hk);
-    vnext.fetch(V + row * a.v_stride, a.v_stride, rows_in(c), col < a.dv);
+    vnext.fetch(V + row * a.v_stride, a.v_stride, vlane, vcol, rows_in(c));
   };
   if (chunks > 0) {
     fetch(0);
@@ -451,48 +594,59 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
     const long row = b + (long)c * C;
     const int count = rows_in(c);
     if (c + 1 < chunks) fetch(c + 1);
-    if (c0 < a.dv) {
-      if (a.carry && c % 2 == 0) S.store(a, a.carry + a.carry_states + state_at(a, (size_t)(first + c / 2), h), col);
-      Frag<3> op[KT];
-#pragma unroll
-      for (int f = 0; f < KT; ++f) op[f] = S.operand(f);
+    if (m.any) {
+      if (OUT && a.carry && c % 2 == 0) S.store(a.carry + a.carry_states + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
       v4f ks[2] = {}, oq[2] = {};
 #pragma unroll
-      for (int f = 0; f < KT; ++f)
+      for (int f = 0; f < KT; ++f) {
+        const Frag<3> op = S.operand(f);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          ks[r] = mma<3>(t.k.along_row(16 * r + c16, f), op[f], ks[r]);
-          oq[r] = mma<PO>(op[f], t.q.along_row(16 * r + c16, f), oq[r]);
+          ks[r] = mma<3>(t.k.along_row(16 * r + c16, f), op, ks[r]);
+          if constexpr (OUT) oq[r] = mma<PO>(op, t.q.along_row(16 * r + c16, f), oq[r]);
         }
+      }
+      const Eight grow(t.grow), beta(t.beta), rest(t.rest);
       float x[8], y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        x[k] = widen(v.v[k]) - t.grow[chunk_row(k)] * ks[k / 4][k % 4];
-        y[k] = t.beta[chunk_row(k)] * x[k];
+        x[k] = (m.map ? 0.f : widen(v.v[k])) - grow[k] * ks[k / 4][k % 4];
+        y[k] = beta[k] * x[k];
       }
       const Frag<3> rb = split8<3>(y);
       v4f nr[2] = {};
 #pragma unroll
       for (int r = 0; r < 2; ++r) nr[r] = mma<3>(t.n.along_row(16 * r + c16, 0), rb, nr[r]);
 #pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] -= nr[k / 4][k % 4];
+      if (OUT && a.carry && col < a.dv) {
+        const size_t wide = (size_t)a.heads * a.dv;
+        float* E = a.carry + row * wide + (size_t)h * a.dv;
+        const unsigned at = (4u * q * (unsigned)wide + col) * 4u;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (count == C || chunk_row(k) < count) *past(E + ((k / 4) * 16 + k % 4) * wide, at) = x[k];
+      }
+#pragma unroll
       for (int k = 0; k < 8; ++k) {
-        x[k] -= nr[k / 4][k % 4];
-        if (a.carry && col < a.dv && chunk_row(k) < count) a.carry[(row + chunk_row(k)) * ((size_t)a.heads * a.dv) + (size_t)h * a.dv + col] = x[k];
-        x[k] *= t.beta[chunk_row(k)];
-        y[k] = t.rest[chunk_row(k)] * x[k];
+        x[k] *= beta[k];
+        y[k] = rest[k] * x[k];
       }
       const Frag<3> up = split8<3>(y);
       const float whole = t.whole;
 #pragma unroll
-      for (int m = 0; m < 2 * KT; ++m) S.t[m] = mma<3>(t.k.down(m, 0), up, S.t[m] * whole);
-      if (a.o) {
-        const Frag<PO> vo = split8<PO>(x);
+      for (int i = 0; i < 2 * KT; ++i) S.t[i] = mma<3>(t.k.down(i, 0), up, S.t[i] * whole);
+      if constexpr (OUT) {
+        if (a.o) {
+          const Frag<PO> vo = split8<PO>(x);
+          T* O = (T*)a.o + row * a.o_stride + (size_t)h * a.dv + m.c0;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          oq[r] = mma<PO>(vo, t.p.along_row(16 * r + c16, 0), oq[r] * (t.grow[16 * r + c16] * a.scale));
-          if (16 * r + c16 < count) {
-            const float o[4] = {oq[r][0], oq[r][1], oq[r][2], oq[r][3]};
-            store_vec((T*)a.o + (row + 16 * r + c16) * a.o_stride + (size_t)h * a.dv + c0 + 4 * q, pack<T>(o), a.dv - c0 - 4 * q);
+          for (int r = 0; r < 2; ++r) {
+            oq[r] = mma<PO>(vo, t.p.along_row(16 * r + c16, 0), oq[r] * (t.grow[16 * r + c16] * a.scale));
+            if (16 * r + c16 < count) {
+              const float o[4] = {oq[r][0], oq[r][1], oq[r][2], oq[r][3]};
+              store_vec(past(O, ((16u * r + c16) * (unsigned)a.o_stride + 4 * q) * (unsigned)sizeof(T)), pack<T>(o), a.dv - m.c0 - 4 * q);
+            }
           }
         }
       }
@@ -503,32 +657,48 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
     }
     __syncthreads();
   }
-  if (a.last) S.store(a, a.last + state_at(a, s, h), col);
+  if (OUT) {
+    if (a.last && w.last) S.store(a.last + state_at(a, w.s, h), a.dk, a.dv, col);
+  } else if (m.map) {
+    S.store(map_of(a, segment, h), a.dk, a.dk, col);
+  } else {
+    S.store(front_of(a, segment + 1, h), a.dk, a.dv, col);
+  }
 }
 
-template <class T, int KT, int W>
+// The same for the gradients, from the last chunk to the first: X and the gradients of the states behind the blocks; or the segments'
+// maps from the gradient behind them to the one in front.
+template <class T, int KT, int W, bool OUT>
 __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
-  typedef Chunk<T, KT, W, 3> Ck;
+  typedef Chunk<T, KT, W, 3, true> Ck;
   constexpr int P = In<T>::P;
   __shared__ typename Ck::Shared sh[2];
   const int h = blockIdx.x % a.heads, hk = h / (a.heads / a.key_heads);
-  const size_t s = blockIdx.x / a.heads;
-  const int lane = threadIdx.x % 64, c16 = lane % 16, c0 = (blockIdx.y * W + threadIdx.x / 64) * 16, col = c0 + c16;
+  const size_t segment = blockIdx.x / a.heads;
+  const int lane = threadIdx.x % 64, c16 = lane % 16, q = lane / 16;
+  Job w;
+  if (!find_job(a, segment, w) || (!OUT && w.first)) return;
+  const Columns m(a, W, !OUT && !w.last);
+  const int col = m.col;
   long b, e;
-  span(a, s, b, e);
-  const long first = first_block(a, s), all = first_block(a, s + 1);
-  if (e > b + (all - first) * B) e = b + (all - first) * B;
+  span(a, w.s, b, e);
+  const long first = first_block(a, w.s) + w.from;
+  b += w.from * B;
+  if (e > b + (w.to - w.from) * B) e = b + (w.to - w.from) * B;
   State<KT> S;   // the gradient of the state behind a chunk
-  S.load(a, a.dlast ? a.dlast + state_at(a, s, h) : nullptr, col);
-  const T* D = (const T*)a.dout + (size_t)h * a.dv + col;
+  if (w.last) S.load(a.dlast ? a.dlast + state_at(a, w.s, h) : nullptr, a.dk, a.dv, col);
+  else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
+  else S.identity(m.map ? col : -1);
+  const T* D = (const T*)a.dout + (size_t)h * a.dv;
+  const unsigned dcol = m.map || col >= a.dv ? 0 : col, dlane = (4u * q * (unsigned)a.dout_stride + dcol) * (unsigned)sizeof(T);
   const int chunks = (int)((e - b + C - 1) / C);
   const auto rows_in = [&](int c) { return e - b - (long)c * C < C ? (int)(e - b - (long)c * C) : C; };
-  Ck next;
+  Ck next(a);
   Rows8<T> dnext;
   const auto fetch = [&](int c) {
     const long row = b + (long)c * C;
     next.fetch(a, row, rows_in(c), (size_t)(first + c / 2), c % 2, h, hk);
-    dnext.fetch(D + row * a.dout_stride, a.dout_stride, rows_in(c), col < a.dv);
+    dnext.fetch(D + row * a.dout_stride, a.dout_stride, dlane, dcol, rows_in(c));
   };
   if (chunks > 0) {
     fetch(chunks - 1);
@@ -541,8 +711,8 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     const long row = b + (long)c * C;
     const int count = rows_in(c);
     if (c > 0) fetch(c - 1);
-    if (c0 < a.dv) {
-      if (c % 2 || c == chunks - 1) S.store(a, a.behind + state_at(a, (size_t)(first + c / 2), h), col);
+    if (m.any) {
+      if (OUT && (c % 2 || c == chunks - 1)) S.store(a.behind + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
       v4f ks[2] = {};
 #pragma unroll
       for (int f = 0; f < KT; ++f) {
@@ -550,14 +720,15 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) ks[r] = mma<3>(t.k.along_row(16 * r + c16, f), op, ks[r]);
       }
+      const Eight grow(t.grow), beta(t.beta), rest(t.rest);
       float x[8], y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = widen(d.v[k]);
+      for (int k = 0; k < 8; ++k) x[k] = m.map ? 0.f : widen(d.v[k]);
       const Frag<P> dop = split8<P>(x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        ks[k / 4][k % 4] *= t.rest[chunk_row(k)];
-        y[k] = a.scale * t.grow[chunk_row(k)] * x[k];
+        ks[k / 4][k % 4] *= rest[k];
+        y[k] = a.scale * grow[k] * x[k];
       }
       const Frag<3> od = split8<3>(y);
 #pragma unroll
@@ -565,22 +736,28 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = ks[k / 4][k % 4];
-        y[k] = t.beta[chunk_row(k)] * x[k];
+        y[k] = beta[k] * x[k];
       }
       const Frag<3> z = split8<3>(y);
       v4f nz[2] = {};
 #pragma unroll
       for (int r = 0; r < 2; ++r) nz[r] = mma<3>(t.n.down(r, 0), z, nz[r]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[k] -= nz[k / 4][k % 4];
-        if (col < a.dv && chunk_row(k) < count) a.x[(row + chunk_row(k)) * ((size_t)a.heads * a.dv) + (size_t)h * a.dv + col] = x[k];
-        y[k] = -t.grow[chunk_row(k)] * t.beta[chunk_row(k)] * x[k];
+      for (int k = 0; k < 8; ++k) x[k] -= nz[k / 4][k % 4];
+      if (OUT && col < a.dv) {
+        const size_t wide = (size_t)a.heads * a.dv;
+        float* X = a.x + row * wide + (size_t)h * a.dv;
+        const unsigned at = (4u * q * (unsigned)wide + col) * 4u;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (count == C || chunk_row(k) < count) *past(X + ((k / 4) * 16 + k % 4) * wide, at) = x[k];
       }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = -grow[k] * beta[k] * x[k];
       const Frag<3> kd = split8<3>(y);
       const float whole = t.whole;
 #pragma unroll
-      for (int m = 0; m < 2 * KT; ++m) S.t[m] = mma<3>(t.k.down(m, 0), kd, mma<3>(t.q.down(m, 0), od, S.t[m] * whole));
+      for (int i = 0; i < 2 * KT; ++i) S.t[i] = mma<3>(t.k.down(i, 0), kd, mma<3>(t.q.down(i, 0), od, S.t[i] * whole));
     }
     if (c > 0) {
       next.put(sh[(c - 1) & 1]);
@@ -588,7 +765,49 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     }
     __syncthreads();
   }
-  if (a.dh0) S.store(a, a.dh0 + state_at(a, s, h), col);
+  if (OUT) {
+    if (a.dh0 && w.first) S.store(a.dh0 + state_at(a, w.s, h), a.dk, a.dv, col);
+  } else if (m.map) {
+    S.store(map_of(a, segment, h), a.dk, a.dk, col);
+  } else {
+    S.store(front_of(a, segment - 1, h), a.dk, a.dv, col);
+  }
+}
+
+// From segment to segment: the state in front of the next (backward: the gradient behind the one before) is the map's share of this one's and what
+// the segment leaves of no state, which lies there already.
+template <int KT, int W, bool BACK>
+__global__ __launch_bounds__(64 * W) void delta_join_kernel(DeltaArgs a) {
+  const int h = blockIdx.x % a.heads, c16 = threadIdx.x % 16, q = threadIdx.x % 64 / 16;
+  const size_t s = blockIdx.x / a.heads;
+  const long size = a.begin ? a.first_segment[a.n_seq + 1] : a.segment, blocks = first_block(a, s + 1) - first_block(a, s);
+  const long count = blocks > size ? (blocks + size - 1) / size : 1;
+  if (count < 3) return;
+  const Columns m(a, W, false);
+  if (!m.any) return;
+  const size_t base = first_segment(a, s);
+  State<KT> S;
+  S.load(front_of(a, base + (BACK ? count - 2 : 1), h), a.dk, a.dv, m.col);
+  for (long j = 1; j + 1 < count; ++j) {
+    const size_t at = base + (BACK ? count - 1 - j : j), to = BACK ? at - 1 : at + 1;
+    const float* map = map_of(a, at, h);
+    State<KT> next;
+    next.load(front_of(a, to, h), a.dk, a.dv, m.col);
+#pragma unroll
+    for (int f = 0; f < KT; ++f) {
+      const Frag<3> op = S.operand(f);
+#pragma unroll
+      for (int i = 0; i < 2 * KT; ++i) {
+        const int r = 16 * i + c16, k0 = 32 * f + 4 * q;
+        const Vec<float, 4> lo = load_group<4>(map + (r < a.dk && k0 < a.dk ? r * a.dk + k0 : 0), r < a.dk ? a.dk - k0 : 0);
+        const Vec<float, 4> hi = load_group<4>(map + (r < a.dk && k0 + 16 < a.dk ? r * a.dk + k0 + 16 : 0), r < a.dk ? a.dk - k0 - 16 : 0);
+        const float x[8] = {get(lo, 0), get(lo, 1), get(lo, 2), get(lo, 3), get(hi, 0), get(hi, 1), get(hi, 2), get(hi, 3)};
+        next.t[i] = mma<3>(split8<3>(x), op, next.t[i]);
+      }
+    }
+    next.store(front_of(a, to, h), a.dk, a.dv, m.col);
+    S = next;
+  }
 }
 
 // ------------------------------------------------------------------ the gradients of a block
@@ -900,11 +1119,12 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
 
 // ------------------------------------------------------------------ launches
 struct Sizes {
-  size_t blocks, first, matrices, sums, x, behind, bytes;   // offsets into the workspace
+  size_t blocks, segments, first, first_segment, matrices, scalars, sums, x, behind, fronts, maps, bytes;   // offsets into the workspace
 };
 Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, bool backward) {
   Sizes s;
   s.blocks = rows / B + (n < rows ? n : rows);
+  s.segments = rows / B >= 24 ? s.blocks / DELTA_SEGMENT + n : 0;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t p = at;
@@ -912,29 +1132,48 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, bool b
     return p;
   };
   s.first = take((n + 1) * sizeof(int));
+  s.first_segment = take((n + 2) * sizeof(int));
   s.matrices = take(s.blocks * heads * 4 * C * C * sizeof(float));
+  s.scalars = take(s.blocks * heads * 4 * B * sizeof(float));
   s.sums = take(s.blocks * heads * B * sizeof(double));
   s.x = take(backward ? rows * heads * dv * sizeof(float) : 0);
   s.behind = take(backward ? s.blocks * heads * dk * dv * sizeof(float) : 0);
+  s.fronts = take(s.segments * heads * dk * dv * sizeof(float));
+  s.maps = take(s.segments * heads * dk * dk * sizeof(float));
   s.bytes = at;
   return s;
 }
+
+// Workgroups that a sequence and head's columns take.
+unsigned groups_of(size_t tiles) { return tiles <= 4 ? 1 : (unsigned)((tiles + 7) / 8); }
 
 void lay_out(DeltaArgs& a, bool backward) {
   const Sizes s = sizes_of(a.rows, a.n_seq, a.heads, a.dk, a.dv, backward);
   char* w = (char*)a.workspace;
   a.blocks = s.blocks;
+  a.segments = s.segments;
   a.first = (int*)(w + s.first);
+  a.first_segment = (int*)(w + s.first_segment);
   a.matrices = (float*)(w + s.matrices);
+  a.scalars = (float*)(w + s.scalars);
   a.sums = (double*)(w + s.sums);
   a.x = (float*)(w + s.x);
   a.behind = (float*)(w + s.behind);
+  a.fronts = (float*)(w + s.fronts);
+  a.maps = (float*)(w + s.maps);
   a.carry_states = a.rows * a.heads * a.dv;
 }
 
-hipError_t plan(const DeltaArgs& a, hipStream_t stream) {
+hipError_t plan(DeltaArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
-  if (a.begin) e = launch(delta_plan_kernel, dim3(1), dim3(PLAN), 0, stream, a);
+  const long work = (long)a.heads * groups_of((a.dv + 15) / 16);
+  if (a.begin) {
+    e = launch(delta_plan_kernel, dim3(1), dim3(PLAN), 0, stream, a, work);
+  } else if (a.segments) {
+    const long blocks = (long)((a.rows + B - 1) / B);
+    a.segment = segment_blocks(blocks, blocks, work);
+    a.segments = a.n_seq && blocks > a.segment ? (size_t)((blocks + a.segment - 1) / a.segment) : 0;
+  }
   const size_t groups = (a.rows + 3) / 4;
   if (e == hipSuccess && a.zero_others && a.rows && (a.begin || !a.n_seq))
     e = launch(delta_zero_kernel, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, stream, a);
@@ -946,14 +1185,29 @@ hipError_t prepare(const DeltaArgs& a, hipStream_t stream) {
   return launch(delta_prepare_kernel<T, KT>, dim3((unsigned)(a.blocks * a.heads)), dim3(256), 0, stream, a);
 }
 
+// The chain: where sequences may be long, the segments' maps and their join in front of it.
+template <class T, int KT, int W, bool BACK>
+hipError_t chain(const DeltaArgs& a, hipStream_t stream) {
+  const unsigned x = (unsigned)((a.segments ? a.segments : a.n_seq) * a.heads), values = (a.dv + 15) / 16, keys = (a.dk + 15) / 16;
+  const auto groups = [](unsigned tiles) { return (tiles + W - 1) / W; };
+  hipError_t e = hipSuccess;
+  if (a.segments) {
+    if constexpr (BACK) e = launch(delta_backward_kernel<T, KT, W, false>, dim3(x, groups(values + keys)), dim3(64 * W), 0, stream, a);
+    else e = launch(delta_forward_kernel<T, KT, W, false>, dim3(x, groups(values + keys)), dim3(64 * W), 0, stream, a);
+    if (e == hipSuccess)
+      e = launch(delta_join_kernel<KT, W, BACK>, dim3((unsigned)(a.n_seq * a.heads), groups(values)), dim3(64 * W), 0, stream, a);
+  }
+  if (e != hipSuccess) return e;
+  if constexpr (BACK) return launch(delta_backward_kernel<T, KT, W, true>, dim3(x, groups(values)), dim3(64 * W), 0, stream, a);
+  else return launch(delta_forward_kernel<T, KT, W, true>, dim3(x, groups(values)), dim3(64 * W), 0, stream, a);
+}
+
 template <class T, int KT>
 hipError_t forward(const DeltaArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.blocks) e = prepare<T, KT>(a, stream);
   if (e != hipSuccess || !a.n_seq) return e;
-  const unsigned x = (unsigned)(a.n_seq * a.heads), tiles = (a.dv + 15) / 16;
-  if (tiles <= 4) return launch(delta_forward_kernel<T, KT, 4>, dim3(x, 1), dim3(256), 0, stream, a);
-  return launch(delta_forward_kernel<T, KT, 8>, dim3(x, (tiles + 7) / 8), dim3(512), 0, stream, a);
+  return a.dv <= 64 ? chain<T, KT, 4, false>(a, stream) : chain<T, KT, 8, false>(a, stream);
 }
 
 template <class T, int KT>
@@ -961,9 +1215,7 @@ hipError_t backward(const DeltaArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.blocks) e = prepare<T, KT>(a, stream);
   if (e != hipSuccess || !a.n_seq) return e;
-  const unsigned x = (unsigned)(a.n_seq * a.heads), tiles = (a.dv + 15) / 16;
-  if (tiles <= 4) e = launch(delta_backward_kernel<T, KT, 4>, dim3(x, 1), dim3(256), 0, stream, a);
-  else e = launch(delta_backward_kernel<T, KT, 8>, dim3(x, (tiles + 7) / 8), dim3(512), 0, stream, a);
+  e = a.dv <= 64 ? chain<T, KT, 4, true>(a, stream) : chain<T, KT, 8, true>(a, stream);
   if (e != hipSuccess || !a.blocks) return e;
   return launch(delta_gradient_kernel<T, KT>, dim3((unsigned)(a.blocks * a.key_heads)), dim3(512), 0, stream, a);
 }

@@ -114,7 +114,7 @@ int check_scan_size(const char* what, int dtype, size_t rows, size_t hidden) {
   return AMP_OK;
 }
 
-// The scan's kernels reach a tile's rows by 32-bit offsets.
+// The recurrences' kernels reach a tile's rows by 32-bit offsets.
 int check_scan_stride(const char* what, const char* name, size_t stride) {
   return stride < (size_t)1 << 22 ? AMP_OK : fail(AMP_EINVAL, "%s: %s has a row stride of 2^22 or more", what, name);
 }
@@ -156,6 +156,8 @@ int check_delta_shape(const char* what, const amp_delta_shape* s, size_t n) {
   if (s->dk < 1 || s->dk > DELTA_MAX_KEY) return fail(AMP_EINVAL, "%s: dk = %zu, 1 .. %d are taken", what, s->dk, DELTA_MAX_KEY);
   if (s->dv < 1 || s->dv > 1024) return fail(AMP_EINVAL, "%s: dv = %zu, 1 .. 1024 are taken", what, s->dv);
   if (n >= MAX_ROWS) return fail(AMP_EINVAL, "%s: %zu sequences, fewer than 2^31 are taken", what, n);
+  if (s->heads * s->dv >= (size_t)1 << 22 || s->key_heads * s->dk >= (size_t)1 << 22)
+    return fail(AMP_EINVAL, "%s: rows of heads x dv or key_heads x dk = 2^22 elements or more", what);
   // a launch has fewer than 2^32 threads, a workgroup to a block or a sequence, and a head
   if ((s->rows / DELTA_BLOCK + n) * s->heads > (size_t)1 << 22)
     return fail(AMP_EINVAL, "%s: %zu rows in %zu sequences of %zu heads, up to 2^22 of (rows / %d + sequences) heads are taken", what, s->rows, n,
@@ -444,6 +446,10 @@ int amp_gated_delta_forward(const amp_delta_shape* shape, const void* q, size_t 
                     {"beta", beta, rows, heads, beta_stride, 4},  {"h0", h0, n, state, state, 4},
                     {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
   CHECK(check_arrays(what, s, 4));
+  CHECK(check_scan_stride(what, "q", q_stride));
+  CHECK(check_scan_stride(what, "k", k_stride));
+  CHECK(check_scan_stride(what, "v", v_stride));
+  CHECK(check_scan_stride(what, "o", o_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 4, nullptr, 0));
   DeltaArgs a = {};
@@ -490,6 +496,10 @@ int amp_gated_delta_backward(const amp_delta_shape* shape, const void* dout, siz
                     {"carry", carry, 1, nc, nc, 4},                     {"dlast", dlast, n, state, state, 4},
                     {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
   CHECK(check_arrays(what, s, 7));
+  CHECK(check_scan_stride(what, "dout", dout_stride));
+  CHECK(check_scan_stride(what, "q", q_stride));
+  CHECK(check_scan_stride(what, "k", k_stride));
+  CHECK(check_scan_stride(what, "v", v_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 7, nullptr, 0));
   DeltaArgs a = {};

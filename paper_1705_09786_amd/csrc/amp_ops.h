@@ -60,6 +60,7 @@ struct DistillArgs {
 
 #define DELTA_CHUNK 32   // rows whose errors are solved for together
 #define DELTA_BLOCK 64   // rows between two states that the backward pass starts from
+#define DELTA_SEGMENT 8  // blocks of the shortest segments that a long sequence is cut into
 #define DELTA_MAX_KEY 128
 
 struct DeltaZero {   // an output whose rows of no sequence become zeros: bytes between rows, 16-bit halves of a row
@@ -86,9 +87,10 @@ struct DeltaArgs {
   void* workspace;
   DeltaZero zero[5];
   // set by the launchers: the workspace's parts, and where the carry's states begin
-  size_t blocks, carry_states;
-  int* first;
-  float *matrices, *x, *behind;
+  size_t blocks, carry_states, segments;   // segments: at most, 0 = sequences stay whole
+  long segment;                            // blocks of one, where there is no plan
+  int *first, *first_segment;
+  float *matrices, *scalars, *x, *behind, *fronts, *maps;
   double* sums;
 };
 

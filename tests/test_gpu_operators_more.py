@@ -200,21 +200,46 @@ def test_delta_step(dtype, rows, heads, key_heads, dk, dv):
     check("last", last, want[1])
 
 
-def test_delta_long_memory_offsets_past_32_bits():
-    """Rows further apart than 2^31 elements."""
-    x, y = layer(3, 1, 1, 1, 8, 8, torch.bfloat16)
-    stride = (1 << 30) + 24
-    wide = torch.empty(2 * stride + 64, dtype=torch.bfloat16, device="cuda")
+def test_delta_offsets_past_32_bits():
+    """Rows of an array of more than 2^31 elements: sequences at its two ends."""
+    n, stride = 700, (1 << 22) - 8
+    x, y = layer(n, 2, 1, 1, 8, 8, torch.bfloat16)
+    begin, end = torch.tensor([0, 660]), torch.tensor([35, 700])
+    wide = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda")
     args = [t.cuda() for t in x.values()]
     for i in (0, 1, 2):
-        view = wide.as_strided((3, 8), (stride, 1), 16 * i)
+        view = wide.as_strided((n, 8), (stride, 1), 16 * i)
         view.copy_(args[i])
         args[i] = view
-    o = wide.as_strided((3, 8), (stride, 1), 48)
-    out, last, _ = ops.gated_delta(*args, h0=dev(y["h0"]), last=True, out=o)
-    want = more.delta(*x.values(), None, 1, None, y["h0"], torch.bfloat16)
-    check("o", out, want[0])
-    check("last", last, want[1])
+    o, do = (wide.as_strided((n, 8), (stride, 1), at) for at in (48, 64))
+    do.copy_(y["do"])
+    got = ops.gated_delta(*args, (begin.cuda(), end.cuda()), h0=dev(y["h0"]), last=True, carry=True, out=o)
+    inside = torch.zeros(n, dtype=torch.bool)
+    inside[:35] = inside[660:] = True
+    want = more.delta(*x.values(), (begin, end), 1, None, y["h0"], torch.bfloat16)
+    check("o", got[0][inside.cuda()], tuple(t[inside] for t in want[0]))
+    check("last", got[1], want[1])
+    back = tuple(wide.as_strided((n, 8), (stride, 1), at) for at in (80, 96, 112)) + tuple(torch.zeros(n, 1, device="cuda") for _ in range(2))
+    grads = ops.gated_delta_backward(do, *args, got[2], (begin.cuda(), end.cuda()), dlast=dev(y["dlast"]), out=back)
+    want = more.delta_backward(y["do"], *x.values(), (begin, end), 1, None, y["h0"], y["dlast"], torch.bfloat16)
+    for name, g, w in zip(NAMES, grads, want):
+        if g.dim() == 2:
+            g, w = g[inside.cuda()], tuple(t[inside] for t in w)
+        check(name, g, w)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sequences", [None, (2000, 0, 3, 2300), (5, 1700, 1800, 64)])
+def test_delta_sequences_cut_into_segments(dtype, sequences):
+    """One head and long sequences: segments side by side, joined from their maps. States that hardly fade carry errors far."""
+    rows = 3000 if sequences is None else sum(sequences)
+    n = 1 if sequences is None else len(sequences)
+    x, y = layer(rows, n, 1, 1, 24, 20, dtype, decay=0.001)
+    x["decay"][rows // 2] = -INF
+    where = None if sequences is None else offsets(*sequences)
+    got = both(x, y, where, 1)
+    against(x, y, where, 1, got)
+    assert all(same_bits(p, q) for p, q in zip(got, both(x, y, where, 1)))
 
 
 # ------------------------------------------------------------------ policy loss

@@ -72,6 +72,11 @@ def test_delta_shape_refusals():
             refused(f(**{name: None}), name + " is NULL")
             refused(f(**{name: AT[name] + 2}), "aligned")
             refused(f(**{name + "_stride": 1 << 60}), "spans")
+        refused(f(heads=32768, key_heads=1, dv=128), "2^22")
+        refused(f(heads=32768, key_heads=32768, dk=128), "2^22")
+    for f, names in ((forward, ("q", "k", "v", "o")), (backward, ("q", "k", "v", "dout"))):
+        for name in names:
+            refused(f(**{name + "_stride": 1 << 22}), "2^22")
     refused(forward(null=True), "shape is NULL")
     refused(forward(seq=(1 << 22, P, P, 8, 0)), "2^22")
 
