@@ -42,32 +42,34 @@ struct Frag {
   v4u p[P];
 };
 
-template <int P>
-__device__ __forceinline__ void split2(float a, float b, unsigned (&u)[P]) {
+// N pairs of numbers in parts: u[part][pair].
+template <int P, int N>
+__device__ __forceinline__ void split(float (&a)[N], float (&b)[N], unsigned (&u)[P][N]) {
   // what a part leaves of its number, exactly, in one instruction: a - 1 u.lo - 0 u.hi. (The factors pass through registers: as a
-  // constant -1 the instruction would take the upper half.)
+  // constant -1 the instruction would take the upper half.) Part by part over all pairs: its result is late for the next instruction.
   unsigned lo = 0xbf80u, hi = 0xbf800000u;
   asm("" : "+s"(lo));
   asm("" : "+s"(hi));
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    u[i] = pack2(a, b, bf16());
-    if (i + 1 < P) {
-      a = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i]), __builtin_bit_cast(v2bf, lo), a, false);
-      b = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i]), __builtin_bit_cast(v2bf, hi), b, false);
-    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) u[i][k] = pack2(a[k], b[k], bf16());
+    if (i + 1 < P)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        a[k] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i][k]), __builtin_bit_cast(v2bf, lo), a[k], false);
+        b[k] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u[i][k]), __builtin_bit_cast(v2bf, hi), b[k], false);
+      }
   }
 }
 template <int P>
 __device__ __forceinline__ Frag<P> split8(const float (&x)[8]) {
+  float a[4] = {x[0], x[2], x[4], x[6]}, b[4] = {x[1], x[3], x[5], x[7]};
+  unsigned u[P][4];
+  split<P, 4>(a, b, u);
   Frag<P> f;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    unsigned u[P];
-    split2<P>(x[2 * k], x[2 * k + 1], u);
-#pragma unroll
-    for (int i = 0; i < P; ++i) f.p[i][k] = u[i];
-  }
+  for (int i = 0; i < P; ++i) f.p[i] = (v4u){u[i][0], u[i][1], u[i][2], u[i][3]};
   return f;
 }
 
@@ -83,29 +85,45 @@ __device__ __forceinline__ v4f mma(const Frag<PA>& a, const Frag<PB>& b, v4f c) 
   return c;
 }
 
-// Matrices in LDS: parts, rows, LD elements a row. Their columns lie in fours; of 32 columns the fours 0, 4, 1, 5, 2, 6, 3, 7 are next to
-// each other (`place`), so that a lane's eight along a row, columns 4 q .. and 16 + 4 q .., are 16 bytes.
-__device__ __forceinline__ int place(int four) { return (four / 8) * 32 + (four % 4) * 8 + (four / 4 % 2) * 4; }
-
-template <int P, int ROWS, int LD>
-struct Matrix {
-  alignas(16) bf16 at[P][ROWS][LD];
-  // the operand whose lane has row `row`, contracted over the columns 32 f ..
-  __device__ __forceinline__ Frag<P> along_row(int row, int f) const {
-    Frag<P> r;
+// The same for two operands a side by side, whose results wait for nothing of one another.
+template <int ORDER, int PA, int PB>
+__device__ __forceinline__ void mma2(const Frag<PA> (&a)[2], const Frag<PB>& b, v4f (&c)[2]) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) r.p[i] = *(const v4u*)&at[i][row][f * 32 + (threadIdx.x % 64 / 16) * 8];
-    return r;
-  }
-  // the operand whose lane has column 16 tile + lane % 16, contracted over the rows row0 ..: read transposed, four rows of 16 columns
-  // to 16 lanes
-  __device__ __forceinline__ Frag<P> down(int tile, int row0) const {
-    const int lane = threadIdx.x % 64, q = lane / 16, row = row0 + 4 * q + lane % 16 / 4, col = place(4 * tile + lane % 4);
+  for (int s = ORDER - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+      if (s - i >= 0 && s - i < PB)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          c[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a[r].p[i]), __builtin_bit_cast(v8bf, b.p[s - i]), c[r], 0, 0, 0);
+}
+
+// Matrices in LDS. An operand is read along its rows, 8 bytes from each of 16 rows at a time, or down its columns, transposed, 32 bytes from each of
+// four rows: rows 8 words more than a multiple of 32 apart, and 2 between fours of them, put either's 16 lanes on 32 banks of their own.
+template <int P, int ROWS, int COLS>
+struct Matrix {
+  static constexpr int LD = COLS + 16;
+  alignas(16) bf16 at[P][ROWS * LD + 16];
+  static __device__ __forceinline__ int place(int row, int col) { return row * LD + row / 4 % 4 * 4 + col; }
+  // the operand whose lane has row row0 + lane % 16, contracted over the columns 32 f ..: 4 q .. and 16 + 4 q ..
+  __device__ __forceinline__ Frag<P> along(int row0, int f) const {
+    const int o = place(row0 + threadIdx.x % 16, 32 * f + threadIdx.x % 64 / 16 * 4);
     Frag<P> r;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)&at[i][row][col]));
-      const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)&at[i][row + 16][col]));
+      const v2u lo = *(const v2u*)&at[i][o], hi = *(const v2u*)&at[i][o + 16];
+      r.p[i] = (v4u){lo.x, lo.y, hi.x, hi.y};
+    }
+    return r;
+  }
+  // the operand whose lane has column 16 tile + lane % 16, contracted over the rows row0 ..: four rows of 16 columns to 16 lanes
+  __device__ __forceinline__ Frag<P> down(int tile, int row0) const {
+    const int lane = threadIdx.x % 64, row = row0 + lane / 16 * 4 + lane % 16 / 4, col = 16 * tile + 4 * (lane % 4);
+    Frag<P> r;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)&at[i][place(row, col)]));
+      const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)&at[i][place(row + 16, col)]));
       r.p[i] = (v4u){lo.x, lo.y, hi.x, hi.y};
     }
     return r;
@@ -113,17 +131,20 @@ struct Matrix {
   // four columns from 4 `four` on
   __device__ __forceinline__ void put(int row, int four, const v2u (&u)[P]) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) *(v2u*)&at[i][row][place(four)] = u[i];
+    for (int i = 0; i < P; ++i) *(v2u*)&at[i][place(row, 4 * four)] = u[i];
   }
 };
 
+// Nothing moves across: the reads in front are on their way while what follows is worked on.
+__device__ __forceinline__ void on_their_way() { __builtin_amdgcn_sched_barrier(0); }
+
 template <int P>
 __device__ __forceinline__ void split4(const float (&x)[4], v2u (&u)[P]) {
-  unsigned a[P], b[P];
-  split2<P>(x[0], x[1], a);
-  split2<P>(x[2], x[3], b);
+  float a[2] = {x[0], x[2]}, b[2] = {x[1], x[3]};
+  unsigned w[P][2];
+  split<P, 2>(a, b, w);
 #pragma unroll
-  for (int i = 0; i < P; ++i) u[i] = (v2u){a[i], b[i]};
+  for (int i = 0; i < P; ++i) u[i] = (v2u){w[i][0], w[i][1]};
 }
 __device__ __forceinline__ void parts4(const Vec<bf16, 4>& v, v2u (&u)[1]) { u[0] = v.u; }
 template <class T, int P>
@@ -298,8 +319,8 @@ __global__ __launch_bounds__(256) void delta_zero_kernel(DeltaArgs a) {
 // ------------------------------------------------------------------ per block and head: N, P and the sums of decays
 template <class T, int KT>
 __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
-  constexpr int P = In<T>::P, LD = KT * 32 + 8;
-  __shared__ Matrix<P, B, LD> k, q;
+  constexpr int P = In<T>::P;
+  __shared__ Matrix<P, B, KT * 32> k, q;
   __shared__ float mat[2][2][C][C + 4];   // chunk, K K^T or Q K^T
   __shared__ double g[B];
   __shared__ float beta[B];
@@ -346,12 +367,12 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
   __syncthreads();
   {   // a wave to each product of each chunk: its three tiles that have elements on or below the diagonal
     const int chunk = wave / 2, r0 = chunk * C, c = lane % 16;
-    const Matrix<P, B, LD>& left = wave % 2 ? q : k;
+    const Matrix<P, B, KT * 32>& left = wave % 2 ? q : k;
     v4f acc[3] = {};
 #pragma unroll
     for (int f = 0; f < KT; ++f) {
-      const Frag<P> a0 = left.along_row(r0 + c, f), a1 = left.along_row(r0 + 16 + c, f);
-      const Frag<P> b0 = k.along_row(r0 + c, f), b1 = k.along_row(r0 + 16 + c, f);
+      const Frag<P> a0 = left.along(r0, f), a1 = left.along(r0 + 16, f);
+      const Frag<P> b0 = k.along(r0, f), b1 = k.along(r0 + 16, f);
       acc[0] = mma<3>(a0, b0, acc[0]);
       acc[1] = mma<3>(a1, b0, acc[1]);
       acc[2] = mma<3>(a1, b1, acc[2]);
@@ -398,13 +419,13 @@ __device__ __forceinline__ T* past(T* base, unsigned bytes) { return (T*)((char*
 // What a chunk's waves share, on its way from memory and in LDS. OUT: with Q and P (in PN parts), else K and N alone.
 template <class T, int KT, int W, int PN, bool OUT>
 struct Chunk {
-  static constexpr int P = In<T>::P, LD = KT * 32 + 8, UNITS = C * KT * 8, STEP = 64 * W / (KT * 8), PER = (UNITS + 64 * W - 1) / (64 * W);
+  static constexpr int P = In<T>::P, UNITS = C * KT * 8, STEP = 64 * W / (KT * 8), PER = (UNITS + 64 * W - 1) / (64 * W);
   static constexpr int FOURS = (OUT ? 2 : 1) * C * C / 4, PAIR = (FOURS + 64 * W - 1) / (64 * W);
   struct Shared {
-    Matrix<P, C, LD> k;
-    Matrix<OUT ? P : 1, OUT ? C : 1, OUT ? LD : 8> q;
-    Matrix<3, C, C + 8> n;
-    Matrix<PN, OUT ? C : 1, C + 8> p;
+    Matrix<P, C, KT * 32> k;
+    Matrix<OUT ? P : 1, OUT ? C : 1, KT * 32> q;
+    Matrix<3, C, C> n;
+    Matrix<PN, OUT ? C : 1, C> p;
     alignas(16) float grow[C], rest[C], beta[C], whole;
   };
   Vec<T, 4> k[PER], q[OUT ? PER : 1];
@@ -597,16 +618,40 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
     if (m.any) {
       if (OUT && a.carry && c % 2 == 0) S.store(a.carry + a.carry_states + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
       v4f ks[2] = {}, oq[2] = {};
-#pragma unroll
-      for (int f = 0; f < KT; ++f) {
-        const Frag<3> op = S.operand(f);
+      Frag<In<T>::P> kf[2][2], qf[2][2];
+      const auto read = [&](int f) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          ks[r] = mma<3>(t.k.along_row(16 * r + c16, f), op, ks[r]);
-          if constexpr (OUT) oq[r] = mma<PO>(op, t.q.along_row(16 * r + c16, f), oq[r]);
+          kf[f % 2][r] = t.k.along(16 * r, f);
+          if constexpr (OUT) qf[f % 2][r] = t.q.along(16 * r, f);
         }
-      }
+      };
+      read(0);
       const Eight grow(t.grow), beta(t.beta), rest(t.rest);
+      const float whole = t.whole;
+      Frag<3> nf[2];
+#pragma unroll
+      for (int f = 0; f < KT; ++f) {
+        if (f + 1 < KT) read(f + 1);
+        else
+#pragma unroll
+          for (int r = 0; r < 2; ++r) nf[r] = t.n.along(16 * r, 0);
+        on_their_way();
+        const v4f decayed[2] = {S.t[2 * f] * whole, S.t[2 * f + 1] * whole};
+        const Frag<3> op = S.operand(f);
+        S.t[2 * f] = decayed[0], S.t[2 * f + 1] = decayed[1];
+        mma2<3>(kf[f % 2], op, ks);
+        if constexpr (OUT)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) oq[r] = mma<PO>(op, qf[f % 2][r], oq[r]);
+      }
+      Frag<In<T>::P> kd[2];
+      kd[0] = t.k.down(0, 0);
+      Frag<PO> pf[2];
+      if constexpr (OUT)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) pf[r] = t.p.along(16 * r, 0);
+      on_their_way();
       float x[8], y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -615,8 +660,7 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
       }
       const Frag<3> rb = split8<3>(y);
       v4f nr[2] = {};
-#pragma unroll
-      for (int r = 0; r < 2; ++r) nr[r] = mma<3>(t.n.along_row(16 * r + c16, 0), rb, nr[r]);
+      mma2<3>(nf, rb, nr);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] -= nr[k / 4][k % 4];
       if (OUT && a.carry && col < a.dv) {
@@ -633,16 +677,19 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
         y[k] = rest[k] * x[k];
       }
       const Frag<3> up = split8<3>(y);
-      const float whole = t.whole;
 #pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) S.t[i] = mma<3>(t.k.down(i, 0), up, S.t[i] * whole);
+      for (int i = 0; i < 2 * KT; ++i) {
+        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0);
+        on_their_way();
+        S.t[i] = mma<3>(kd[i % 2], up, S.t[i]);
+      }
       if constexpr (OUT) {
         if (a.o) {
           const Frag<PO> vo = split8<PO>(x);
           T* O = (T*)a.o + row * a.o_stride + (size_t)h * a.dv + m.c0;
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            oq[r] = mma<PO>(vo, t.p.along_row(16 * r + c16, 0), oq[r] * (t.grow[16 * r + c16] * a.scale));
+            oq[r] = mma<PO>(vo, pf[r], oq[r] * (t.grow[16 * r + c16] * a.scale));
             if (16 * r + c16 < count) {
               const float o[4] = {oq[r][0], oq[r][1], oq[r][2], oq[r][3]};
               store_vec(past(O, ((16u * r + c16) * (unsigned)a.o_stride + 4 * q) * (unsigned)sizeof(T)), pack<T>(o), a.dv - m.c0 - 4 * q);
@@ -714,13 +761,30 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     if (m.any) {
       if (OUT && (c % 2 || c == chunks - 1)) S.store(a.behind + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
       v4f ks[2] = {};
+      Frag<P> kf[2][2];
+      const auto read = [&](int f) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) kf[f % 2][r] = t.k.along(16 * r, f);
+      };
+      read(0);
+      const Eight grow(t.grow), beta(t.beta), rest(t.rest);
+      const float whole = t.whole;
+      Frag<3> pf[2], nf[2];
 #pragma unroll
       for (int f = 0; f < KT; ++f) {
-        const Frag<3> op = S.operand(f);
+        if (f + 1 < KT) read(f + 1);
+        else
 #pragma unroll
-        for (int r = 0; r < 2; ++r) ks[r] = mma<3>(t.k.along_row(16 * r + c16, f), op, ks[r]);
+          for (int r = 0; r < 2; ++r) pf[r] = t.p.down(r, 0);
+        on_their_way();
+        const v4f decayed[2] = {S.t[2 * f] * whole, S.t[2 * f + 1] * whole};
+        const Frag<3> op = S.operand(f);
+        S.t[2 * f] = decayed[0], S.t[2 * f + 1] = decayed[1];
+        mma2<3>(kf[f % 2], op, ks);
       }
-      const Eight grow(t.grow), beta(t.beta), rest(t.rest);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) nf[r] = t.n.down(r, 0);
+      on_their_way();
       float x[8], y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = m.map ? 0.f : widen(d.v[k]);
@@ -731,8 +795,10 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
         y[k] = a.scale * grow[k] * x[k];
       }
       const Frag<3> od = split8<3>(y);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) ks[r] = mma<3>(t.p.down(r, 0), dop, ks[r]);
+      mma2<3>(pf, dop, ks);
+      Frag<P> kd[2], qd[2];
+      kd[0] = t.k.down(0, 0), qd[0] = t.q.down(0, 0);
+      on_their_way();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = ks[k / 4][k % 4];
@@ -740,8 +806,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       }
       const Frag<3> z = split8<3>(y);
       v4f nz[2] = {};
-#pragma unroll
-      for (int r = 0; r < 2; ++r) nz[r] = mma<3>(t.n.down(r, 0), z, nz[r]);
+      mma2<3>(nf, z, nz);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] -= nz[k / 4][k % 4];
       if (OUT && col < a.dv) {
@@ -754,10 +819,13 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] = -grow[k] * beta[k] * x[k];
-      const Frag<3> kd = split8<3>(y);
-      const float whole = t.whole;
+      const Frag<3> down = split8<3>(y);
 #pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) S.t[i] = mma<3>(t.k.down(i, 0), kd, mma<3>(t.q.down(i, 0), od, S.t[i] * whole));
+      for (int i = 0; i < 2 * KT; ++i) {
+        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0), qd[(i + 1) % 2] = t.q.down(i + 1, 0);
+        on_their_way();
+        S.t[i] = mma<3>(kd[i % 2], down, mma<3>(qd[i % 2], od, S.t[i]));
+      }
     }
     if (c > 0) {
       next.put(sh[(c - 1) & 1]);
@@ -811,21 +879,21 @@ __global__ __launch_bounds__(64 * W) void delta_join_kernel(DeltaArgs a) {
 }
 
 // ------------------------------------------------------------------ the gradients of a block
-// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other.
+// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other. Values, their gradients and the states
+// pass in steps of 32 columns, the next step on its way meanwhile, its operands in the other half of the LDS.
 template <class T, int KT>
 __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
-  constexpr int P = In<T>::P, LD = KT * 32 + 8, LV = 32 + 8, LB = B + 8;
-  struct Step {   // 32 columns of the values
-    alignas(16) bf16 d[P][B][LV], y[3][B][LV], w[3][B][LV];
-  };
+  constexpr int P = In<T>::P, LV = 32 + 8, Y = P, W = P + 3, PLANES = P + 6;
+  constexpr bool KEEP = P < 3;   // there is room for K and Q
+  typedef bf16 Plane[B][LV];
   struct Pair {
-    alignas(16) bf16 p[3][B][LB], m[3][B][LB];
+    Matrix<3, B, B> p, m;
   };
   __shared__ union {
-    Step s;
-    Pair m;
+    alignas(16) Plane step[2][PLANES];   // dO, beta X, beta E
+    Pair pair;
   } u;
-  __shared__ Matrix<P, B, LD> kq;
+  __shared__ Matrix<P, B, KT * 32> kq[KEEP ? 2 : 1];
   __shared__ double g[B];
   __shared__ float grow[B], rest[B], beta[B], dots[8][B], ends[8];
   Block w;
@@ -836,45 +904,53 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   const int kc = 16 * wave + c16;   // the column of dq and dk
   const T* K = row_of((const T*)a.k, w.row, a.k_stride) + (size_t)hk * a.dk;
   const T* Q = row_of((const T*)a.q, w.row, a.q_stride) + (size_t)hk * a.dk;
-  const auto load_kq = [&](const T* p, size_t stride) {
+  const auto load_kq = [&](const T* p, size_t stride, Matrix<P, B, KT * 32>& to) {
 #pragma unroll
     for (int j = 0; j < B * KT * 8 / 512; ++j) {
       const int i = threadIdx.x + j * 512, row = i / (KT * 8), four = i % (KT * 8);
       const long n = row < w.count ? a.dk - four * 4 : 0;
       v2u x[P];
       parts4(load_group<4>(p + (n > 0 ? row * stride + four * 4 : 0), n), x);
-      kq.put(row, four, x);
+      to.put(row, four, x);
     }
   };
-  // operands in LDS whose columns lie in their order
-  const auto along = [&](const auto& m, int row) {   // contracted over a step's 32 columns, eight of them in a row
-    constexpr int PP = sizeof(m) / sizeof(m[0]);
-    Frag<PP> r;
+  if (KEEP) {
+    load_kq(K, a.k_stride, kq[0]);
+    load_kq(Q, a.q_stride, kq[KEEP ? 1 : 0]);
+  }
+  const size_t wide = (size_t)a.heads * a.dv;
+  const int row = threadIdx.x / 8;
+  const bool in = row < w.count;
+  const size_t r = in ? w.row + row : w.row;
+  const T* D = (const T*)a.dout + r * a.dout_stride;
+  const float *E = a.carry_in + r * wide, *X = a.x + r * wide;
+  // a step on its way: four of a row's values, eight of the lane's rows of both states
+  Vec<T, 4> d;
+  Vec<float, 4> ev, xv;
+  Vec<float, 4> s0[2], s1[2];
+  const auto fetch = [&](int h, int v0) {
+    const long n = in ? a.dv - v0 - 4 * (int)(threadIdx.x % 8) : 0;
+    const size_t at = n > 0 ? (size_t)h * a.dv + v0 + 4 * (threadIdx.x % 8) : 0;
+    d = load_group<4>(D + at, n);
+    ev = load_group<4>(E + at, n), xv = load_group<4>(X + at, n);
+    const bool mine = owner && kc < a.dk;
+    const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h);
+    const float* behind = a.behind + state_at(a, w.index, h);
 #pragma unroll
-    for (int i = 0; i < PP; ++i) r.p[i] = *(const v4u*)&m[i][row][8 * q];
-    return r;
-  };
-  const auto over_rows = [&](const bf16 (&m)[3][B][LB], int row, int f) {   // as `down` has its rows
-    Frag<3> r;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const v2u lo = *(const v2u*)&m[i][row][32 * f + 4 * q], hi = *(const v2u*)&m[i][row][32 * f + 16 + 4 * q];
-      r.p[i] = (v4u){lo.x, lo.y, hi.x, hi.y};
+    for (int k = 0; k < 2; ++k) {
+      const long left = mine ? a.dv - v0 - 8 * q - 4 * k : 0;
+      const size_t o = left > 0 ? (size_t)kc * a.dv + v0 + 8 * q + 4 * k : 0;
+      s0[k] = load_group<4>(before + o, left), s1[k] = load_group<4>(behind + o, left);
     }
-    return r;
   };
-  const auto turned = [&](const bf16 (&m)[3][B][LB], int tile, int f) {
-    Frag<3> r;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const bf16* p = &m[i][32 * f + 4 * q + c16 / 4][16 * tile + 4 * (lane % 4)];
-      const v2u lo = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p));
-      const v2u hi = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 16 * LB)));
-      r.p[i] = (v4u){lo.x, lo.y, hi.x, hi.y};
-    }
-    return r;
+  // which tiles on and below the diagonal of dO W^T (0 .. 9) and Y W^T (10 .. 19) are the wave's
+  const auto tile_of = [](int o, int& it, int& jt) {
+    it = o >= 6 ? 3 : o >= 3 ? 2 : o >= 1 ? 1 : 0;
+    jt = o - it * (it + 1) / 2;
   };
+  fetch(hk * group, 0);
   v4f sum_q[4] = {}, sum_k[4] = {};
+  int turn = 0;
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
     __syncthreads();   // the head in front is done with LDS
     if (threadIdx.x < B) {
@@ -883,142 +959,170 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       g[threadIdx.x] = mine;
       grow[threadIdx.x] = expf((float)mine);
       rest[threadIdx.x] = expf((float)(end - mine));
-      beta[threadIdx.x] = (int)threadIdx.x < w.count ? a.beta[(w.row + threadIdx.x) * a.beta_stride + h] : 0.f;
+      beta[threadIdx.x] = scalars_of(a, w.index, h)[2 * B + threadIdx.x];
     }
     __syncthreads();
-    const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h);
-    const float* behind = a.behind + state_at(a, w.index, h);
-    const size_t wide = (size_t)a.heads * a.dv;
     v4f dq[4] = {}, dr[4] = {}, dc[4] = {};   // by the rows' own decays: q's, k's where it reads the state, k's where it writes it
-    v4f pair[3] = {};                         // tiles of dO W^T (0 .. 9) and Y W^T (10 .. 19) on and below the diagonal
+    v4f pair[3] = {};
     float ss = 0.f, dbeta = 0.f;
-    const int row = threadIdx.x / 8;
-    const bool in = row < w.count;
-    for (int v0 = 0; v0 < a.dv; v0 += 32) {
-      const long n = in ? a.dv - v0 - 4 * (int)(threadIdx.x % 8) : 0;
-      const size_t at = n > 0 ? (size_t)h * a.dv + v0 + 4 * (threadIdx.x % 8) : 0;
-      const size_t r = in ? w.row + row : w.row;
-      const Vec<T, 4> d = load_group<4>((const T*)a.dout + r * a.dout_stride + at, n);
-      const Vec<float, 4> ev = load_group<4>(a.carry_in + r * wide + at, n), xv = load_group<4>(a.x + r * wide + at, n);
-      float s0[8] = {}, s1[8] = {};
-      if (kc < a.dk && owner) {
-        const long left = a.dv - v0 - 8 * q;
-#pragma unroll
-        for (int k = 0; k < 8; k += 4) {
-          const size_t o = left > k ? (size_t)kc * a.dv + v0 + 8 * q + k : 0;
-          const Vec<float, 4> x = load_group<4>(before + o, left - k), y = load_group<4>(behind + o, left - k);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s0[k + i] = get(x, i), s1[k + i] = get(y, i);
-        }
-      }
+    for (int v0 = 0; v0 < a.dv; v0 += 32, turn ^= 1) {
+      Plane* s = u.step[turn];
+      const int col = 4 * (threadIdx.x % 8);
+      const float b = beta[row];
       float y[4], e[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         dbeta = fmaf(get(xv, i), get(ev, i), dbeta);
-        y[i] = beta[row] * get(xv, i);
-        e[i] = beta[row] * get(ev, i);
+        y[i] = b * get(xv, i);
+        e[i] = b * get(ev, i);
       }
-      if (n > 0) store_vec((T*)a.dvalue + r * a.dv_stride + at, pack<T>(y), n);
+      const long n = in ? a.dv - v0 - col : 0;
+      if (n > 0) store_vec((T*)a.dvalue + r * a.dv_stride + (size_t)h * a.dv + v0 + col, pack<T>(y), n);
       v2u x[3], z[P];
       parts4(d, z);
 #pragma unroll
-      for (int i = 0; i < P; ++i) *(v2u*)&u.s.d[i][row][4 * (threadIdx.x % 8)] = z[i];
+      for (int i = 0; i < P; ++i) *(v2u*)&s[i][row][col] = z[i];
       split4<3>(y, x);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) *(v2u*)&u.s.y[i][row][4 * (threadIdx.x % 8)] = x[i];
+      for (int i = 0; i < 3; ++i) *(v2u*)&s[Y + i][row][col] = x[i];
       split4<3>(e, x);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) *(v2u*)&u.s.w[i][row][4 * (threadIdx.x % 8)] = x[i];
-      __syncthreads();
-      if (owner) {
-        const Frag<3> f0 = split8<3>(s0), f1 = split8<3>(s1);
+      for (int i = 0; i < 3; ++i) *(v2u*)&s[W + i][row][col] = x[i];
+      float f0[8], f1[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) ss = fmaf(s0[k], s1[k], ss);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          dq[t] = mma<3>(along(u.s.d, 16 * t + c16), f0, dq[t]);
-          dr[t] = mma<3>(along(u.s.y, 16 * t + c16), f0, dr[t]);
-          dc[t] = mma<3>(along(u.s.w, 16 * t + c16), f1, dc[t]);
-        }
+      for (int k = 0; k < 8; ++k) {
+        f0[k] = get(s0[k / 4], k % 4), f1[k] = get(s1[k / 4], k % 4);
+        ss = fmaf(f0[k], f1[k], ss);
       }
+      if (v0 + 32 < a.dv) fetch(h, v0 + 32);
+      else if (h + 1 < (hk + 1) * group) fetch(h + 1, 0);
+      __syncthreads();
+      // one part of four tiles of rows after the other, the four side by side
+      const auto times = [&](int plane, int parts, const Frag<3>& f, v4f(&c)[4]) {
+#pragma unroll
+        for (int i = parts - 1; i >= 0; --i) {
+          v8bf op[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) op[t] = *(const v8bf*)&s[plane + i][16 * t + c16][8 * q];
+#pragma unroll
+          for (int j = 2 - i; j >= 0; --j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[t], __builtin_bit_cast(v8bf, f.p[j]), c[t], 0, 0, 0);
+        }
+      };
+      if (owner) {
+        const Frag<3> before = split8<3>(f0), behind = split8<3>(f1);
+        times(0, P, before, dq);
+        times(Y, 3, before, dr);
+        times(W, 3, behind, dc);
+      }
+      const auto operand = [&](int plane, auto& f, int r0) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(f.p) / sizeof(f.p[0])); ++i) f.p[i] = *(const v4u*)&s[plane + i][r0 + c16][8 * q];
+      };
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        const int t = wave + 8 * k, o = t % 10, it = o >= 6 ? 3 : o >= 3 ? 2 : o >= 1 ? 1 : 0, jt = o - it * (it + 1) / 2;
-        if (t < 10) pair[k] = mma<3>(along(u.s.d, 16 * it + c16), along(u.s.w, 16 * jt + c16), pair[k]);
-        else if (t < 20) pair[k] = mma<3>(along(u.s.y, 16 * it + c16), along(u.s.w, 16 * jt + c16), pair[k]);
-      }
-      __syncthreads();
-    }
-    // dbeta: the eight threads of a row
-    dbeta = group_sum<8>(dbeta);
-    if (in && threadIdx.x % 8 == 0) a.dbeta[(w.row + row) * a.dbeta_stride + h] = dbeta;
-    // the pairs' gradients into LDS, and zeros above the diagonal where an operand has them
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int t = wave + 8 * k, o = t % 10, it = o >= 6 ? 3 : o >= 3 ? 2 : o >= 1 ? 1 : 0, jt = o - it * (it + 1) / 2;
-      if (t >= 24) continue;
-      const int zero = t - 20;   // 20 .. 23: the tiles (0, 1) and (2, 3) of both
-      const int i0 = 16 * (zero >= 0 ? zero / 2 * 2 : it), j = 16 * (zero >= 0 ? zero / 2 * 2 + 1 : jt) + c16;
-      bf16(*m)[B][LB] = (zero >= 0 ? zero % 2 : t >= 10) ? u.m.m : u.m.p;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = i0 + 4 * q + i;
-        float x = 0.f;
-        if (zero < 0 && t < 10 && r >= j) x = a.scale * expf((float)(g[r] - g[j])) * pair[k][i];
-        if (zero < 0 && t >= 10 && r > j) x = -expf((float)(g[r] - g[j])) * pair[k][i];
-        unsigned p[3];
-        split2<3>(x, 0.f, p);
-#pragma unroll
-        for (int z = 0; z < 3; ++z) *(unsigned short*)&m[z][r][j] = (unsigned short)p[z];
+        const int t = wave + 8 * k;
+        int it, jt;
+        tile_of(t % 10, it, jt);
+        Frag<3> right;
+        if (t < 20) operand(W, right, 16 * jt);
+        if (t < 10) {
+          Frag<P> left;
+          operand(0, left, 16 * it);
+          pair[k] = mma<3>(left, right, pair[k]);
+        } else if (t < 20) {
+          Frag<3> left;
+          operand(Y, left, 16 * it);
+          pair[k] = mma<3>(left, right, pair[k]);
+        }
       }
     }
-    float tail = 0.f;   // what the sum of all decays of the block is owed
-    v4f kv[4], qv[4];
+    T kv[4][4], qv[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = 16 * t + 4 * q + i;
         const bool there = owner && kc < a.dk && r < w.count;
-        kv[t][i] = there ? widen(K[r * a.k_stride + kc]) : 0.f;
-        qv[t][i] = there ? widen(Q[r * a.q_stride + kc]) : 0.f;
-        dq[t][i] *= a.scale * grow[r];
-        dr[t][i] *= -grow[r];
-        dc[t][i] *= rest[r];
-        tail = fmaf(kv[t][i], dc[t][i], tail);
+        kv[t][i] = qv[t][i] = (T)0.f;
+        if (there) kv[t][i] = K[r * a.k_stride + kc], qv[t][i] = Q[r * a.q_stride + kc];
       }
-    tail = group_sum<64>(fmaf(expf((float)g[B - 1]), ss, tail));
-    if (lane == 0) ends[wave] = tail;
-    load_kq(Q, a.q_stride);
+    // dbeta: the eight threads of a row
+    dbeta = group_sum<8>(dbeta);
+    if (in && threadIdx.x % 8 == 0) a.dbeta[(w.row + row) * a.dbeta_stride + h] = dbeta;
     __syncthreads();
-    if (owner)
+    // the pairs' gradients into LDS, and zeros above the diagonal where an operand has them
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const Frag<P> b = kq.down(wave, 32 * f);
+    for (int k = 0; k < 3; ++k) {
+      const int t = wave + 8 * k, zero = t - 20;   // 20 .. 23: the tiles (0, 1) and (2, 3) of both
+      int it, jt;
+      tile_of(t % 10, it, jt);
+      const int i0 = 16 * (zero >= 0 ? zero / 2 * 2 : it), j = 16 * (zero >= 0 ? zero / 2 * 2 + 1 : jt) + c16;
+      const bool second = zero >= 0 ? zero % 2 : t >= 10;
+      float x[4], none[4] = {};
 #pragma unroll
-        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(turned(u.m.p, t, f), b, dc[t]);
+      for (int i = 0; i < 4; ++i) {
+        const int r = i0 + 4 * q + i;
+        const bool there = zero < 0 && (second ? r > j : r >= j);
+        x[i] = there ? (second ? -1.f : a.scale) * expf((float)(g[r] - g[j])) * pair[k][i] : 0.f;
       }
-    __syncthreads();
-    load_kq(K, a.k_stride);
-    __syncthreads();
-    if (owner) {
+      unsigned p[3][4];
+      split<3, 4>(x, none, p);
+      Matrix<3, B, B>& m = second ? u.pair.m : u.pair.p;
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const Frag<P> b = kq.down(wave, 32 * f);
+      for (int z = 0; z < 3; ++z)
 #pragma unroll
-        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(turned(u.m.m, t, f), b, dc[t]);
-#pragma unroll
-        for (int t = 2 * f; t < 4; ++t) {
-          dq[t] = mma<3>(over_rows(u.m.p, 16 * t + c16, f), b, dq[t]);
-          dr[t] = mma<3>(over_rows(u.m.m, 16 * t + c16, f), b, dr[t]);
-        }
-      }
+        for (int i = 0; i < 4; ++i) *(unsigned short*)&m.at[z][m.place(i0 + 4 * q + i, j)] = (unsigned short)p[z][i];
     }
+    float tail = 0.f;   // what the sum of all decays of the block is owed
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = group_sum<16>(qv[t][i] * dq[t][i] + kv[t][i] * (dr[t][i] - dc[t][i]));
+        const int r = 16 * t + 4 * q + i;
+        dq[t][i] *= a.scale * grow[r];
+        dr[t][i] *= -grow[r];
+        dc[t][i] *= rest[r];
+        tail = fmaf(widen(kv[t][i]), dc[t][i], tail);
+      }
+    tail = group_sum<64>(fmaf(expf((float)g[B - 1]), ss, tail));
+    if (lane == 0) ends[wave] = tail;
+    if (!KEEP) load_kq(Q, a.q_stride, kq[0]);
+    __syncthreads();
+    const auto with_q = [&](const Matrix<P, B, KT * 32>& m) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Frag<P> b = m.down(wave, 32 * f);
+#pragma unroll
+        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(u.pair.p.down(t, 32 * f), b, dc[t]);
+      }
+    };
+    const auto with_k = [&](const Matrix<P, B, KT * 32>& m) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Frag<P> b = m.down(wave, 32 * f);
+#pragma unroll
+        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(u.pair.m.down(t, 32 * f), b, dc[t]);
+#pragma unroll
+        for (int t = 2 * f; t < 4; ++t) {
+          dq[t] = mma<3>(u.pair.p.along(16 * t, f), b, dq[t]);
+          dr[t] = mma<3>(u.pair.m.along(16 * t, f), b, dr[t]);
+        }
+      }
+    };
+    if (owner) with_q(kq[KEEP ? 1 : 0]);
+    if (!KEEP) {
+      __syncthreads();
+      load_kq(K, a.k_stride, kq[0]);
+      __syncthreads();
+    }
+    if (owner) with_k(kq[0]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = group_sum<16>(widen(qv[t][i]) * dq[t][i] + widen(kv[t][i]) * (dr[t][i] - dc[t][i]));
         if (c16 == 0) dots[wave][16 * t + 4 * q + i] = x;
         sum_q[t][i] += dq[t][i];
         sum_k[t][i] += dr[t][i] + dc[t][i];
