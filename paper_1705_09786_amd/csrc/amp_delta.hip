@@ -153,6 +153,43 @@ __device__ __forceinline__ void parts4(const Vec<T, 4>& v, v2u (&u)[P]) {
   split4<P>(x, u);
 }
 
+// Four elements, n and later replaced by zeros. `fours`, the same for all lanes: n is a multiple of 4, as where dk and dv are. (A branch for
+// every count of elements instead costs the kernels' loops registers, which they spill.) p can be read where n is 0 as well.
+template <class T>
+__device__ __forceinline__ Vec<T, 4> load_four(const T* p, int n, bool fours) {
+  Vec<T, 4> v;
+  v.u = (typename Vec<T, 4>::U)0u;
+  if (fours) {
+    if (n > 0) v.u = *(const typename Vec<T, 4>::Any*)p;
+  } else {
+    unsigned e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const T* at = p + (k < n ? k : 0);
+      const unsigned x = sizeof(T) == 2 ? (unsigned)*(const unsigned short*)at : *(const unsigned*)at;
+      e[k] = k < n ? x : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (sizeof(T) == 2) v.u[k / 2] |= e[k] << (16 * (k & 1));
+      else v.u[k] = e[k];
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void store_four(T* p, Vec<T, 4> v, int n, bool fours) {
+  if (fours) {
+    if (n > 0) *(typename Vec<T, 4>::Any*)p = v.u;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) {
+        if (sizeof(T) == 2) ((unsigned short*)p)[k] = (unsigned short)(v.u[k / 2] >> (16 * (k & 1)));
+        else ((unsigned*)p)[k] = v.u[k];
+      }
+  }
+}
+
 // ------------------------------------------------------------------ where things are
 struct Block {
   long row;      // its first row
@@ -174,7 +211,7 @@ __device__ __forceinline__ void span(const DeltaArgs& a, size_t s, long& b, long
 // Blocks in front of a sequence, at most the workspace's number of them.
 __device__ __forceinline__ long first_block(const DeltaArgs& a, size_t s) { return a.begin ? a.first[s] : s ? (long)a.blocks : 0; }
 
-__device__ __forceinline__ bool find_block(const DeltaArgs& a, size_t index, Block& w) {
+__device__ __forceinline__ bool search_block(const DeltaArgs& a, size_t index, Block& w) {
   size_t lo = 0, hi = a.n_seq;   // first[lo] <= index < first[hi]
   if ((long)index >= first_block(a, hi)) return false;
   while (hi - lo > 1) {
@@ -186,6 +223,13 @@ __device__ __forceinline__ bool find_block(const DeltaArgs& a, size_t index, Blo
   w.row = b + ((long)index - first_block(a, lo)) * B;
   w.count = e - w.row < B ? (int)(e - w.row) : B;
   w.index = index;
+  return w.count > 0;
+}
+
+// The same from the plan's table: a block's first row and its rows, 0 where there is none.
+__device__ __forceinline__ bool find_block(const DeltaArgs& a, size_t index, Block& w) {
+  if (!a.begin) return search_block(a, index, w);
+  w.row = a.table[2 * index], w.count = a.table[2 * index + 1], w.index = index;
   return w.count > 0;
 }
 
@@ -275,6 +319,12 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
   }
   const long all = base < most ? base : most;
   if (threadIdx.x == 0) a.first[a.n_seq] = (int)all;
+  __syncthreads();
+  for (size_t i = threadIdx.x; i < a.blocks; i += PLAN) {
+    Block w;
+    const bool in = search_block(a, i, w);
+    a.table[2 * i] = in ? (int)w.row : 0, a.table[2 * i + 1] = in ? w.count : 0;
+  }
   if (!a.segments) return;
   for (int d = 1; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d, 64));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = longest;
@@ -335,9 +385,9 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
     const int u = threadIdx.x + j * 256, row = u / (KT * 8), four = u % (KT * 8);
     const long n = row < w.count ? a.dk - four * 4 : 0;
     v2u x[P];
-    parts4(load_group<4>(K + (row < w.count ? row : 0) * a.k_stride + (n > 0 ? four * 4 : 0), n), x);
+    parts4(load_four(K + (row < w.count ? row : 0) * a.k_stride + (n > 0 ? four * 4 : 0), n, a.fours), x);
     k.put(row, four, x);
-    parts4(load_group<4>(Q + (row < w.count ? row : 0) * a.q_stride + (n > 0 ? four * 4 : 0), n), x);
+    parts4(load_four(Q + (row < w.count ? row : 0) * a.q_stride + (n > 0 ? four * 4 : 0), n, a.fours), x);
     q.put(row, four, x);
   }
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -448,8 +498,8 @@ struct Chunk {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const bool in = count == C || mine + j * STEP < count;   // rows behind the sequence's end are zeros
-      k[j] = load_group<4>(past(K + (in ? j * STEP * a.k_stride : 0), in ? k0 : 0u), in ? n : 0);
-      if (OUT) q[j] = load_group<4>(past(Q + (in ? j * STEP * a.q_stride : 0), in ? q0 : 0u), in ? n : 0);
+      k[j] = load_four(past(K + (in ? j * STEP * a.k_stride : 0), in ? k0 : 0u), in ? n : 0, a.fours);
+      if (OUT) q[j] = load_four(past(Q + (in ? j * STEP * a.q_stride : 0), in ? q0 : 0u), in ? n : 0, a.fours);
     }
     const float* m = matrices_of(a, block, h, half);
 #pragma unroll
@@ -692,7 +742,7 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
             oq[r] = mma<PO>(vo, pf[r], oq[r] * (t.grow[16 * r + c16] * a.scale));
             if (16 * r + c16 < count) {
               const float o[4] = {oq[r][0], oq[r][1], oq[r][2], oq[r][3]};
-              store_vec(past(O, ((16u * r + c16) * (unsigned)a.o_stride + 4 * q) * (unsigned)sizeof(T)), pack<T>(o), a.dv - m.c0 - 4 * q);
+              store_four(past(O, ((16u * r + c16) * (unsigned)a.o_stride + 4 * q) * (unsigned)sizeof(T)), pack<T>(o), a.dv - m.c0 - 4 * q, a.fours);
             }
           }
         }
@@ -867,8 +917,8 @@ __global__ __launch_bounds__(64 * W) void delta_join_kernel(DeltaArgs a) {
 #pragma unroll
       for (int i = 0; i < 2 * KT; ++i) {
         const int r = 16 * i + c16, k0 = 32 * f + 4 * q;
-        const Vec<float, 4> lo = load_group<4>(map + (r < a.dk && k0 < a.dk ? r * a.dk + k0 : 0), r < a.dk ? a.dk - k0 : 0);
-        const Vec<float, 4> hi = load_group<4>(map + (r < a.dk && k0 + 16 < a.dk ? r * a.dk + k0 + 16 : 0), r < a.dk ? a.dk - k0 - 16 : 0);
+        const Vec<float, 4> lo = load_four(map + (r < a.dk && k0 < a.dk ? r * a.dk + k0 : 0), r < a.dk ? a.dk - k0 : 0, a.fours);
+        const Vec<float, 4> hi = load_four(map + (r < a.dk && k0 + 16 < a.dk ? r * a.dk + k0 + 16 : 0), r < a.dk ? a.dk - k0 - 16 : 0, a.fours);
         const float x[8] = {get(lo, 0), get(lo, 1), get(lo, 2), get(lo, 3), get(hi, 0), get(hi, 1), get(hi, 2), get(hi, 3)};
         next.t[i] = mma<3>(split8<3>(x), op, next.t[i]);
       }
@@ -879,23 +929,38 @@ __global__ __launch_bounds__(64 * W) void delta_join_kernel(DeltaArgs a) {
 }
 
 // ------------------------------------------------------------------ the gradients of a block
-// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other. Values, their gradients and the states
-// pass in steps of 32 columns, the next step on its way meanwhile, its operands in the other half of the LDS.
-template <class T, int KT>
+// With W = beta E, Y = beta X, S and S' the state in front of a block and the gradient behind it, D the decays between its rows, and of a key's heads
+//   dP = sum of scale D o (dO W^T),  dM = sum of -D o (Y W^T)  (on and below, and below the diagonal),
+//   dq = sum of scale e^G dO S^T + dP K,  dk = sum of (e^{G_end - G} W S'^T - e^G Y S^T) + dP^T Q + dM K + dM^T K,  dv = Y.
+// A decay's gradient needs no more products: where all of a state is scaled, what o gains is q.dq, and what v would have to gain for
+// the errors to follow is v.dv, so that G's gradient at a row is q.dq - v.dv, and at the last the state's own, <S', the state behind>, as well.
+// Of q.dq the part of dP is the sum over a row of dP o (Q K^T).
+//
+// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other, their sums kept in the workspace (each
+// thread its own). Values, their gradients and the states pass in steps of 32 columns, the next on its way meanwhile, its operands in the other
+// half of the LDS. What becomes dq and dk alone, which are rounded to the inputs' type, is formed from two parts where that is a type
+// of 16 bits (2^-16 of the terms are left out); what becomes ddecay too, in 32 bits, from all.
+template <class T, int KT, bool FOURS>
 __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
-  constexpr int P = In<T>::P, LV = 32 + 8, Y = P, W = P + 3, PLANES = P + 6;
-  constexpr bool KEEP = P < 3;   // there is room for K and Q
+  constexpr int P = In<T>::P, PK = sizeof(T) == 2 ? 2 : 3, LV = 32 + 8, Y = P, W = P + PK, PLANES = P + PK + 3;
+  constexpr bool KEEP = P < 3;   // there is room for K beside Q
   typedef bf16 Plane[B][LV];
+  struct Rows {
+    float dots[8][B], prow[4][B], ends[8];
+  };
   struct Pair {
-    Matrix<3, B, B> p, m;
+    Matrix<PK, B, B> p, m;
   };
   __shared__ union {
     alignas(16) Plane step[2][PLANES];   // dO, beta X, beta E
+    Rows rows;
     Pair pair;
+    Matrix<P, B, KT * 32> k;
   } u;
-  __shared__ Matrix<P, B, KT * 32> kq[KEEP ? 2 : 1];
+  __shared__ Matrix<P, B, KT * 32> kq;
+  __shared__ Matrix<KEEP ? P : 1, KEEP ? B : 1, KT * 32> kept_k;
   __shared__ double g[B];
-  __shared__ float grow[B], rest[B], beta[B], dots[8][B], ends[8];
+  __shared__ float grow[B], rest[B], beta[B], vrow[B];
   Block w;
   const int hk = blockIdx.x % a.key_heads, group = a.heads / a.key_heads;
   if (!find_block(a, blockIdx.x / a.key_heads, w)) return;
@@ -904,55 +969,71 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   const int kc = 16 * wave + c16;   // the column of dq and dk
   const T* K = row_of((const T*)a.k, w.row, a.k_stride) + (size_t)hk * a.dk;
   const T* Q = row_of((const T*)a.q, w.row, a.q_stride) + (size_t)hk * a.dk;
-  const auto load_kq = [&](const T* p, size_t stride, Matrix<P, B, KT * 32>& to) {
+  const auto load_kq = [&](const T* p, unsigned stride, Matrix<P, B, KT * 32>& to) {
+    Vec<T, 4> x[B * KT * 8 / 512];
 #pragma unroll
     for (int j = 0; j < B * KT * 8 / 512; ++j) {
-      const int i = threadIdx.x + j * 512, row = i / (KT * 8), four = i % (KT * 8);
-      const long n = row < w.count ? a.dk - four * 4 : 0;
-      v2u x[P];
-      parts4(load_group<4>(p + (n > 0 ? row * stride + four * 4 : 0), n), x);
-      to.put(row, four, x);
+      const int i = threadIdx.x + j * 512, row = i / (KT * 8), four = i % (KT * 8), n = row < w.count ? a.dk - four * 4 : 0;
+      x[j] = load_four(past(p, n > 0 ? (row * stride + four * 4) * (unsigned)sizeof(T) : 0u), n, FOURS);
     }
-  };
-  if (KEEP) {
-    load_kq(K, a.k_stride, kq[0]);
-    load_kq(Q, a.q_stride, kq[KEEP ? 1 : 0]);
-  }
-  const size_t wide = (size_t)a.heads * a.dv;
-  const int row = threadIdx.x / 8;
-  const bool in = row < w.count;
-  const size_t r = in ? w.row + row : w.row;
-  const T* D = (const T*)a.dout + r * a.dout_stride;
-  const float *E = a.carry_in + r * wide, *X = a.x + r * wide;
-  // a step on its way: four of a row's values, eight of the lane's rows of both states
-  Vec<T, 4> d;
-  Vec<float, 4> ev, xv;
-  Vec<float, 4> s0[2], s1[2];
-  const auto fetch = [&](int h, int v0) {
-    const long n = in ? a.dv - v0 - 4 * (int)(threadIdx.x % 8) : 0;
-    const size_t at = n > 0 ? (size_t)h * a.dv + v0 + 4 * (threadIdx.x % 8) : 0;
-    d = load_group<4>(D + at, n);
-    ev = load_group<4>(E + at, n), xv = load_group<4>(X + at, n);
-    const bool mine = owner && kc < a.dk;
-    const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h);
-    const float* behind = a.behind + state_at(a, w.index, h);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const long left = mine ? a.dv - v0 - 8 * q - 4 * k : 0;
-      const size_t o = left > 0 ? (size_t)kc * a.dv + v0 + 8 * q + 4 * k : 0;
-      s0[k] = load_group<4>(before + o, left), s1[k] = load_group<4>(behind + o, left);
+    for (int j = 0; j < B * KT * 8 / 512; ++j) {
+      const int i = threadIdx.x + j * 512;
+      v2u y[P];
+      parts4(x[j], y);
+      to.put(i / (KT * 8), i % (KT * 8), y);
     }
   };
-  // which tiles on and below the diagonal of dO W^T (0 .. 9) and Y W^T (10 .. 19) are the wave's
+  // tiles on and below the diagonal: of dO W^T those numbered 0 .. 9, of Y W^T 10 .. 19; a wave has every eighth
   const auto tile_of = [](int o, int& it, int& jt) {
     it = o >= 6 ? 3 : o >= 3 ? 2 : o >= 1 ? 1 : 0;
     jt = o - it * (it + 1) / 2;
   };
+  Matrix<P, B, KT * 32>& km = [&]() -> Matrix<P, B, KT * 32>& {
+    if constexpr (KEEP) return kept_k;
+    else return u.k;
+  }();
+  load_kq(Q, (unsigned)a.q_stride, kq);
+  load_kq(K, (unsigned)a.k_stride, km);
+  __syncthreads();
+  v4f qk[2] = {};   // Q K^T in the wave's tiles of dP
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (wave + 8 * k < 10) {
+      int it, jt;
+      tile_of(wave + 8 * k, it, jt);
+#pragma unroll
+      for (int f = 0; f < KT; ++f) qk[k] = mma<3>(kq.along(16 * it, f), km.along(16 * jt, f), qk[k]);
+    }
+  const size_t wide = (size_t)a.heads * a.dv;
+  const int row = threadIdx.x / 8, col = 4 * (threadIdx.x % 8);
+  const bool in = row < w.count;
+  const unsigned d_at = (row * (unsigned)a.dout_stride + col) * (unsigned)sizeof(T), v_at = (row * (unsigned)a.v_stride + col) * (unsigned)sizeof(T);
+  const unsigned e_at = (row * (unsigned)wide + col) * 4u, s_at = ((unsigned)kc * a.dv + 8 * q) * 4u;
+  Vec<T, 4> d, v;
+  Vec<float, 4> ev, xv, s0[2], s1[2];
+  const auto fetch = [&](int h, int v0) {
+    const int n = in ? a.dv - v0 - col : 0, left = owner && kc < a.dk ? a.dv - v0 - 8 * q : 0;
+    const size_t at = (size_t)h * a.dv + v0;
+    d = load_four(past((const T*)a.dout + w.row * a.dout_stride + at, n > 0 ? d_at : 0u), n, FOURS);
+    v = load_four(past((const T*)a.v + w.row * a.v_stride + at, n > 0 ? v_at : 0u), n, FOURS);
+    ev = load_four(past(a.carry_in + w.row * wide + at, n > 0 ? e_at : 0u), n, FOURS);
+    xv = load_four(past(a.x + w.row * wide + at, n > 0 ? e_at : 0u), n, FOURS);
+    const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h) + v0;
+    const float* behind = a.behind + state_at(a, w.index, h) + v0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      s0[k] = load_four(past(before + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, FOURS);
+      s1[k] = load_four(past(behind + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, FOURS);
+    }
+};
   fetch(hk * group, 0);
-  v4f sum_q[4] = {}, sum_k[4] = {};
   int turn = 0;
+  // the group's sums: dq's and dk's 16 values of this thread, and dP's and dM's 12
+  float* kept = a.kept + ((w.index * a.key_heads + hk) * 44) * 512;
+  v4f dq[4], dr[4], dc[4], pair[3];
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
-    __syncthreads();   // the head in front is done with LDS
+    __syncthreads();   // LDS is free
     if (threadIdx.x < B) {
       const double* sums = sums_of(a, w.index, h);
       const double half = sums[C - 1], end = half + sums[B - 1], mine = sums[threadIdx.x] + (threadIdx.x >= C ? half : 0.0);
@@ -961,177 +1042,185 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       rest[threadIdx.x] = expf((float)(end - mine));
       beta[threadIdx.x] = scalars_of(a, w.index, h)[2 * B + threadIdx.x];
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) dq[t] = dr[t] = dc[t] = (v4f)0.f;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) pair[k] = (v4f)0.f;
+    float ss = 0.f, dbeta = 0.f, dvv = 0.f;
     __syncthreads();
-    v4f dq[4] = {}, dr[4] = {}, dc[4] = {};   // by the rows' own decays: q's, k's where it reads the state, k's where it writes it
-    v4f pair[3] = {};
-    float ss = 0.f, dbeta = 0.f;
     for (int v0 = 0; v0 < a.dv; v0 += 32, turn ^= 1) {
-      Plane* s = u.step[turn];
-      const int col = 4 * (threadIdx.x % 8);
-      const float b = beta[row];
-      float y[4], e[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dbeta = fmaf(get(xv, i), get(ev, i), dbeta);
-        y[i] = b * get(xv, i);
-        e[i] = b * get(ev, i);
-      }
-      const long n = in ? a.dv - v0 - col : 0;
-      if (n > 0) store_vec((T*)a.dvalue + r * a.dv_stride + (size_t)h * a.dv + v0 + col, pack<T>(y), n);
-      v2u x[3], z[P];
-      parts4(d, z);
-#pragma unroll
-      for (int i = 0; i < P; ++i) *(v2u*)&s[i][row][col] = z[i];
-      split4<3>(y, x);
-#pragma unroll
-      for (int i = 0; i < 3; ++i) *(v2u*)&s[Y + i][row][col] = x[i];
-      split4<3>(e, x);
-#pragma unroll
-      for (int i = 0; i < 3; ++i) *(v2u*)&s[W + i][row][col] = x[i];
+      Plane* step = u.step[turn];
       float f0[8], f1[8];
+      {
+        const int n = in ? a.dv - v0 - col : 0;
+        const size_t at = (size_t)h * a.dv + v0;
+        const float b = beta[row];
+        float y[4], e[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        f0[k] = get(s0[k / 4], k % 4), f1[k] = get(s1[k / 4], k % 4);
-        ss = fmaf(f0[k], f1[k], ss);
+        for (int i = 0; i < 4; ++i) {
+          dbeta = fmaf(get(xv, i), get(ev, i), dbeta);
+          y[i] = b * get(xv, i);
+          e[i] = b * get(ev, i);
+          dvv = fmaf(y[i], get(v, i), dvv);
+        }
+        store_four((T*)a.dvalue + (w.row + row) * a.dv_stride + at + col, pack<T>(y), n, FOURS);
+        v2u x[3], yp[PK], z[P];
+        parts4(d, z);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *(v2u*)&step[i][row][col] = z[i];
+        split4<PK>(y, yp);
+#pragma unroll
+        for (int i = 0; i < PK; ++i) *(v2u*)&step[Y + i][row][col] = yp[i];
+        split4<3>(e, x);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *(v2u*)&step[W + i][row][col] = x[i];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          f0[k] = get(s0[k / 4], k % 4), f1[k] = get(s1[k / 4], k % 4);
+          ss = fmaf(f0[k], f1[k], ss);
+        }
       }
       if (v0 + 32 < a.dv) fetch(h, v0 + 32);
       else if (h + 1 < (hk + 1) * group) fetch(h + 1, 0);
       __syncthreads();
       // one part of four tiles of rows after the other, the four side by side
-      const auto times = [&](int plane, int parts, const Frag<3>& f, v4f(&c)[4]) {
+      const auto times = [&](int plane, int parts, int order, const Frag<3>& f, v4f(&c)[4]) {
 #pragma unroll
         for (int i = parts - 1; i >= 0; --i) {
           v8bf op[4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) op[t] = *(const v8bf*)&s[plane + i][16 * t + c16][8 * q];
+          for (int t = 0; t < 4; ++t) op[t] = *(const v8bf*)&step[plane + i][16 * t + c16][8 * q];
 #pragma unroll
-          for (int j = 2 - i; j >= 0; --j)
+          for (int j = order - 1 - i; j >= 0; --j)
 #pragma unroll
             for (int t = 0; t < 4; ++t) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[t], __builtin_bit_cast(v8bf, f.p[j]), c[t], 0, 0, 0);
         }
       };
       if (owner) {
-        const Frag<3> before = split8<3>(f0), behind = split8<3>(f1);
-        times(0, P, before, dq);
-        times(Y, 3, before, dr);
-        times(W, 3, behind, dc);
+        const Frag<3> s = split8<3>(f0);
+        times(0, P, 3, s, dq);
+        times(Y, PK, PK, s, dr);
+        times(W, 3, 3, split8<3>(f1), dc);
       }
       const auto operand = [&](int plane, auto& f, int r0) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(f.p) / sizeof(f.p[0])); ++i) f.p[i] = *(const v4u*)&s[plane + i][r0 + c16][8 * q];
+        for (int i = 0; i < (int)(sizeof(f.p) / sizeof(f.p[0])); ++i) f.p[i] = *(const v4u*)&step[plane + i][r0 + c16][8 * q];
       };
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
         const int t = wave + 8 * k;
         int it, jt;
         tile_of(t % 10, it, jt);
-        Frag<3> right;
-        if (t < 20) operand(W, right, 16 * jt);
         if (t < 10) {
-          Frag<P> left;
-          operand(0, left, 16 * it);
-          pair[k] = mma<3>(left, right, pair[k]);
+          Frag<P> l;
+          Frag<3> r;
+          operand(0, l, 16 * it);
+          operand(W, r, 16 * jt);
+          pair[k] = mma<3>(l, r, pair[k]);
         } else if (t < 20) {
-          Frag<3> left;
-          operand(Y, left, 16 * it);
-          pair[k] = mma<3>(left, right, pair[k]);
+          Frag<PK> l, r;
+          operand(Y, l, 16 * it);
+          operand(W, r, 16 * jt);
+          pair[k] = mma<PK>(l, r, pair[k]);
         }
       }
     }
-    T kv[4][4], qv[4][4];
+    // by row: dbeta and v.dv from the eight threads of one, q.dq from the waves' columns and the tiles of dP. (Addresses of what follows are
+    // formed here, from a thread's number that the compiler takes for another in each turn: in front of the loop they would fill the registers.)
+    unsigned id = threadIdx.x;
+    asm volatile("" : "+v"(id));
+    const int lane = id % 64, wave = id / 64, c16 = lane % 16, q = lane / 16, kc = 16 * wave + c16;
+    const unsigned mine = id * 4u;
+    float kv[KEEP ? 1 : 4][4];
+    if constexpr (!KEEP)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // of the last row and column beyond them: what they meet is 0
+        const int r = 16 * t + 4 * q + i < w.count ? 16 * t + 4 * q + i : w.count - 1, c = kc < a.dk ? kc : a.dk - 1;
+        kv[t][i] = widen(*past(K, ((unsigned)r * (unsigned)a.k_stride + c) * (unsigned)sizeof(T)));
+      }
+    dbeta = group_sum<8>(dbeta), dvv = group_sum<8>(dvv);
+    if (threadIdx.x % 8 == 0) {
+      if (in) a.dbeta[(w.row + row) * a.dbeta_stride + h] = dbeta;
+      vrow[row] = dvv;
+    }
+    __syncthreads();
+    float tail = expf((float)g[B - 1]) * ss;   // <S', the state behind>
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = 16 * t + 4 * q + i;
-        const bool there = owner && kc < a.dk && r < w.count;
-        kv[t][i] = qv[t][i] = (T)0.f;
-        if (there) kv[t][i] = K[r * a.k_stride + kc], qv[t][i] = Q[r * a.q_stride + kc];
+        const float f = grow[r];
+        dq[t][i] *= a.scale * f;
+        const float c = rest[r] * dc[t][i];
+        if constexpr (KEEP) {
+          float y = 0.f;
+          if (owner)
+#pragma unroll
+            for (int z = P - 1; z >= 0; --z) y += widen(km.at[z][km.place(r, kc)]);
+          tail = fmaf(y, c, tail);
+        } else {
+          tail = fmaf(kv[t][i], c, tail);
+        }
+        dr[t][i] = fmaf(-f, dr[t][i], c);   // both of dk's
+        float x = 0.f;
+        if (owner)
+#pragma unroll
+          for (int z = P - 1; z >= 0; --z) x += widen(kq.at[z][kq.place(r, kc)]);
+        x = group_sum<16>(x * dq[t][i]);
+        if (c16 == 0) u.rows.dots[wave][r] = x;
       }
-    // dbeta: the eight threads of a row
-    dbeta = group_sum<8>(dbeta);
-    if (in && threadIdx.x % 8 == 0) a.dbeta[(w.row + row) * a.dbeta_stride + h] = dbeta;
-    __syncthreads();
-    // the pairs' gradients into LDS, and zeros above the diagonal where an operand has them
+    tail = group_sum<64>(tail);
+    if (lane == 0) u.rows.ends[wave] = tail;
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      const int t = wave + 8 * k, zero = t - 20;   // 20 .. 23: the tiles (0, 1) and (2, 3) of both
+      const int t = wave + 8 * k;
+      if (t >= 20) continue;
       int it, jt;
       tile_of(t % 10, it, jt);
-      const int i0 = 16 * (zero >= 0 ? zero / 2 * 2 : it), j = 16 * (zero >= 0 ? zero / 2 * 2 + 1 : jt) + c16;
-      const bool second = zero >= 0 ? zero % 2 : t >= 10;
-      float x[4], none[4] = {};
+      const int j = 16 * jt + c16;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = i0 + 4 * q + i;
-        const bool there = zero < 0 && (second ? r > j : r >= j);
-        x[i] = there ? (second ? -1.f : a.scale) * expf((float)(g[r] - g[j])) * pair[k][i] : 0.f;
-      }
-      unsigned p[3][4];
-      split<3, 4>(x, none, p);
-      Matrix<3, B, B>& m = second ? u.pair.m : u.pair.p;
-#pragma unroll
-      for (int z = 0; z < 3; ++z)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *(unsigned short*)&m.at[z][m.place(i0 + 4 * q + i, j)] = (unsigned short)p[z][i];
-    }
-    float tail = 0.f;   // what the sum of all decays of the block is owed
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * t + 4 * q + i;
-        dq[t][i] *= a.scale * grow[r];
-        dr[t][i] *= -grow[r];
-        dc[t][i] *= rest[r];
-        tail = fmaf(widen(kv[t][i]), dc[t][i], tail);
-      }
-    tail = group_sum<64>(fmaf(expf((float)g[B - 1]), ss, tail));
-    if (lane == 0) ends[wave] = tail;
-    if (!KEEP) load_kq(Q, a.q_stride, kq[0]);
-    __syncthreads();
-    const auto with_q = [&](const Matrix<P, B, KT * 32>& m) {
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const Frag<P> b = m.down(wave, 32 * f);
-#pragma unroll
-        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(u.pair.p.down(t, 32 * f), b, dc[t]);
-      }
-    };
-    const auto with_k = [&](const Matrix<P, B, KT * 32>& m) {
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const Frag<P> b = m.down(wave, 32 * f);
-#pragma unroll
-        for (int t = 0; t < 2 * f + 2; ++t) dc[t] = mma<3>(u.pair.m.down(t, 32 * f), b, dc[t]);
-#pragma unroll
-        for (int t = 2 * f; t < 4; ++t) {
-          dq[t] = mma<3>(u.pair.p.along(16 * t, f), b, dq[t]);
-          dr[t] = mma<3>(u.pair.m.along(16 * t, f), b, dr[t]);
+        const int r = 16 * it + 4 * q + i;
+        const bool there = t >= 10 ? r > j : r >= j;
+        pair[k][i] = there ? (t >= 10 ? -1.f : a.scale) * expf((float)(g[r] - g[j])) * pair[k][i] : 0.f;
+        if (t < 10) {
+          const float y = group_sum<16>(pair[k][i] * qk[k < 2 ? k : 0][i]);
+          if (c16 == 0) u.rows.prow[jt][r] = y;
         }
       }
-    };
-    if (owner) with_q(kq[KEEP ? 1 : 0]);
-    if (!KEEP) {
-      __syncthreads();
-      load_kq(K, a.k_stride, kq[0]);
-      __syncthreads();
     }
-    if (owner) with_k(kq[0]);
+    if (group > 1) {   // to the heads in front
+      if (h > hk * group) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = group_sum<16>(widen(qv[t][i]) * dq[t][i] + widen(kv[t][i]) * (dr[t][i] - dc[t][i]));
-        if (c16 == 0) dots[wave][16 * t + 4 * q + i] = x;
-        sum_q[t][i] += dq[t][i];
-        sum_k[t][i] += dr[t][i] + dc[t][i];
+          for (int i = 0; i < 4; ++i) dq[t][i] += *past(kept + (4 * t + i) * 512, mine), dr[t][i] += *past(kept + (16 + 4 * t + i) * 512, mine);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pair[k][i] += *past(kept + (32 + 4 * k + i) * 512, mine);
       }
+      if (h + 1 < (hk + 1) * group) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *past(kept + (4 * t + i) * 512, mine) = dq[t][i], *past(kept + (16 + 4 * t + i) * 512, mine) = dr[t][i];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *past(kept + (32 + 4 * k + i) * 512, mine) = pair[k][i];
+      }
+    }
     __syncthreads();
     if (wave == 0) {
-      float x = 0.f, end = 0.f;
+      float x = -vrow[lane], end = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x += dots[i][lane], end += ends[i];
+      for (int i = 0; i < 8; ++i) x += u.rows.dots[i][lane], end += u.rows.ends[i];
+      for (int i = 0; i <= lane / 16; ++i) x += u.rows.prow[i][lane];
       if (lane == B - 1) x += end;
 #pragma unroll
       for (int d = 1; d < B; d *= 2) {
@@ -1141,16 +1230,60 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       if (lane < w.count) a.ddecay[(w.row + lane) * a.ddecay_stride + h] = x;
     }
   }
-  if (owner && kc < a.dk)
+  __syncthreads();
+  // dP and dM into LDS, with zeros above the diagonal where an operand has them, and their products
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+  for (int k = 0; k < 3; ++k) {
+    const int t = wave + 8 * k, zero = t - 20;   // 20 .. 23: the tiles (0, 1) and (2, 3) of both
+    int it, jt;
+    tile_of(t % 10, it, jt);
+    const int i0 = 16 * (zero >= 0 ? zero / 2 * 2 : it), j = 16 * (zero >= 0 ? zero / 2 * 2 + 1 : jt) + c16;
+    float x[4], none[4] = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * t + 4 * q + i;
-        if (r >= w.count) continue;
-        ((T*)a.dq)[(w.row + r) * a.dq_stride + (size_t)hk * a.dk + kc] = (T)sum_q[t][i];
-        ((T*)a.dkey)[(w.row + r) * a.dk_stride + (size_t)hk * a.dk + kc] = (T)sum_k[t][i];
-      }
+    for (int i = 0; i < 4; ++i) x[i] = zero >= 0 ? 0.f : pair[k][i];
+    unsigned p[PK][4];
+    split<PK, 4>(x, none, p);
+    Matrix<PK, B, B>& m = (zero >= 0 ? zero % 2 : t >= 10) ? u.pair.m : u.pair.p;
+#pragma unroll
+    for (int z = 0; z < PK; ++z)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(unsigned short*)&m.at[z][m.place(i0 + 4 * q + i, j)] = (unsigned short)p[z][i];
+  }
+  __syncthreads();
+  if (owner)
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const Frag<P> b = kq.down(wave, 32 * f);
+#pragma unroll
+      for (int t = 0; t < 2 * f + 2; ++t) dr[t] = mma<PK>(u.pair.p.down(t, 32 * f), b, dr[t]);
+    }
+  if (!KEEP) {
+    __syncthreads();
+    load_kq(K, (unsigned)a.k_stride, kq);
+    __syncthreads();
+  }
+  if (!owner) return;
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const Frag<P> b = (KEEP ? km : kq).down(wave, 32 * f);
+#pragma unroll
+    for (int t = 0; t < 2 * f + 2; ++t) dr[t] = mma<PK>(u.pair.m.down(t, 32 * f), b, dr[t]);
+#pragma unroll
+    for (int t = 2 * f; t < 4; ++t) {
+      dq[t] = mma<PK>(u.pair.p.along(16 * t, f), b, dq[t]);
+      dr[t] = mma<PK>(u.pair.m.along(16 * t, f), b, dr[t]);
+    }
+  }
+  if (kc >= a.dk) return;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 16 * t + 4 * q + i;
+      if (r >= w.count) continue;
+      ((T*)a.dq)[(w.row + r) * a.dq_stride + (size_t)hk * a.dk + kc] = (T)dq[t][i];
+      ((T*)a.dkey)[(w.row + r) * a.dk_stride + (size_t)hk * a.dk + kc] = (T)dr[t][i];
+    }
 }
 
 // ------------------------------------------------------------------ one row of every sequence
@@ -1223,9 +1356,9 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
 
 // ------------------------------------------------------------------ launches
 struct Sizes {
-  size_t blocks, segments, first, first_segment, matrices, scalars, sums, x, behind, fronts, maps, bytes;   // offsets into the workspace
+  size_t blocks, segments, first, first_segment, table, matrices, scalars, sums, x, behind, kept, fronts, maps, bytes;   // offsets into the workspace
 };
-Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, bool backward) {
+Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk, size_t dv, bool backward) {
   Sizes s;
   s.blocks = rows / B + (n < rows ? n : rows);
   s.segments = rows / B >= 24 ? s.blocks / DELTA_SEGMENT + n : 0;
@@ -1237,11 +1370,13 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, bool b
   };
   s.first = take((n + 1) * sizeof(int));
   s.first_segment = take((n + 2) * sizeof(int));
+  s.table = take(s.blocks * 2 * sizeof(int));
   s.matrices = take(s.blocks * heads * 4 * C * C * sizeof(float));
   s.scalars = take(s.blocks * heads * 4 * B * sizeof(float));
   s.sums = take(s.blocks * heads * B * sizeof(double));
   s.x = take(backward ? rows * heads * dv * sizeof(float) : 0);
   s.behind = take(backward ? s.blocks * heads * dk * dv * sizeof(float) : 0);
+  s.kept = take(backward && heads > key_heads ? s.blocks * key_heads * 44 * 512 * sizeof(float) : 0);
   s.fronts = take(s.segments * heads * dk * dv * sizeof(float));
   s.maps = take(s.segments * heads * dk * dk * sizeof(float));
   s.bytes = at;
@@ -1252,17 +1387,20 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, bool b
 unsigned groups_of(size_t tiles) { return tiles <= 4 ? 1 : (unsigned)((tiles + 7) / 8); }
 
 void lay_out(DeltaArgs& a, bool backward) {
-  const Sizes s = sizes_of(a.rows, a.n_seq, a.heads, a.dk, a.dv, backward);
+  const Sizes s = sizes_of(a.rows, a.n_seq, a.heads, a.key_heads, a.dk, a.dv, backward);
   char* w = (char*)a.workspace;
+  a.fours = a.dk % 4 == 0 && a.dv % 4 == 0;
   a.blocks = s.blocks;
   a.segments = s.segments;
   a.first = (int*)(w + s.first);
   a.first_segment = (int*)(w + s.first_segment);
+  a.table = (int*)(w + s.table);
   a.matrices = (float*)(w + s.matrices);
   a.scalars = (float*)(w + s.scalars);
   a.sums = (double*)(w + s.sums);
   a.x = (float*)(w + s.x);
   a.behind = (float*)(w + s.behind);
+  a.kept = (float*)(w + s.kept);
   a.fronts = (float*)(w + s.fronts);
   a.maps = (float*)(w + s.maps);
   a.carry_states = a.rows * a.heads * a.dv;
@@ -1321,7 +1459,9 @@ hipError_t backward(const DeltaArgs& a, hipStream_t stream) {
   if (e != hipSuccess || !a.n_seq) return e;
   e = a.dv <= 64 ? chain<T, KT, 4, true>(a, stream) : chain<T, KT, 8, true>(a, stream);
   if (e != hipSuccess || !a.blocks) return e;
-  return launch(delta_gradient_kernel<T, KT>, dim3((unsigned)(a.blocks * a.key_heads)), dim3(512), 0, stream, a);
+  const dim3 grid((unsigned)(a.blocks * a.key_heads));
+  if (a.fours) return launch(delta_gradient_kernel<T, KT, true>, grid, dim3(512), 0, stream, a);
+  return launch(delta_gradient_kernel<T, KT, false>, grid, dim3(512), 0, stream, a);
 }
 
 #define BY_KEY(CALL)                  \
@@ -1331,9 +1471,9 @@ hipError_t backward(const DeltaArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-extern "C" size_t amp_delta_blocks(size_t rows, size_t n) { return sizes_of(rows, n, 1, 1, 1, false).blocks; }
-extern "C" size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, int backward) {
-  return sizes_of(rows, n, heads, dk, dv, backward).bytes;
+extern "C" size_t amp_delta_blocks(size_t rows, size_t n) { return sizes_of(rows, n, 1, 1, 1, 1, false).blocks; }
+extern "C" size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk, size_t dv, int backward) {
+  return sizes_of(rows, n, heads, key_heads, dk, dv, backward).bytes;
 }
 
 extern "C" hipError_t amp_delta_forward_launch(int dtype, const DeltaArgs* args, hipStream_t stream) {

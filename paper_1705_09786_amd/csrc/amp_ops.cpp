@@ -417,7 +417,7 @@ int amp_gated_delta_workspace(const amp_delta_shape* s, size_t n, int backward, 
   const char* what = "gated_delta_workspace";
   CHECK(check_delta_shape(what, s, n));
   REQUIRE(bytes);
-  *bytes = amp_delta_workspace_bytes(s->rows, n, s->heads, s->dk, s->dv, backward);
+  *bytes = amp_delta_workspace_bytes(s->rows, n, s->heads, s->key_heads, s->dk, s->dv, backward);
   return AMP_OK;
 }
 
@@ -438,7 +438,7 @@ int amp_gated_delta_forward(const amp_delta_shape* shape, const void* q, size_t 
     REQUIRE(beta);
   }
   const size_t e = elem(shape->dtype), keys = shape->key_heads * shape->dk, values = heads * shape->dv, state = heads * shape->dk * shape->dv;
-  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->dk, shape->dv, 0), nc = delta_carry_floats(shape, n);
+  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->key_heads, shape->dk, shape->dv, 0), nc = delta_carry_floats(shape, n);
   const Span s[] = {{"o", o, rows, values, o_stride, e},          {"last", last, n, state, state, 4},
                     {"carry", carry, 1, nc, nc, 4},               {"workspace", need ? workspace : nullptr, 1, need, need, 1},
                     {"q", q, rows, keys, q_stride, e},            {"k", k, rows, keys, k_stride, e},
@@ -485,7 +485,7 @@ int amp_gated_delta_backward(const amp_delta_shape* shape, const void* dout, siz
     REQUIRE(dbeta);
   }
   const size_t e = elem(shape->dtype), keys = shape->key_heads * shape->dk, values = heads * shape->dv, state = heads * shape->dk * shape->dv;
-  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->dk, shape->dv, 1), nc = delta_carry_floats(shape, n);
+  const size_t need = amp_delta_workspace_bytes(rows, n, heads, shape->key_heads, shape->dk, shape->dv, 1), nc = delta_carry_floats(shape, n);
   const Span s[] = {{"dq", dq, rows, keys, dq_stride, e},               {"dk", dk, rows, keys, dk_stride, e},
                     {"dv", dv, rows, values, dv_stride, e},             {"ddecay", ddecay, rows, heads, ddecay_stride, 4},
                     {"dbeta", dbeta, rows, heads, dbeta_stride, 4},     {"dh0", dh0, n, state, state, 4},

@@ -86,11 +86,12 @@ struct DeltaArgs {
   float *last, *dh0, *carry;
   void* workspace;
   DeltaZero zero[5];
-  // set by the launchers: the workspace's parts, and where the carry's states begin
+  // set by the launchers: whether dk and dv are multiples of 4, the workspace's parts, and where the carry's states begin
+  int fours;
   size_t blocks, carry_states, segments;   // segments: at most, 0 = sequences stay whole
   long segment;                            // blocks of one, where there is no plan
-  int *first, *first_segment;
-  float *matrices, *scalars, *x, *behind, *fronts, *maps;
+  int *first, *first_segment, *table;
+  float *matrices, *scalars, *x, *behind, *kept, *fronts, *maps;
   double* sums;
 };
 
@@ -149,7 +150,7 @@ hipError_t amp_scan_forward_launch(int dtype, int tanh, const ScanArgs* a, hipSt
 hipError_t amp_scan_backward_launch(int dtype, int tanh, const ScanArgs* a, hipStream_t stream);
 hipError_t amp_scan_step_launch(int dtype, int tanh, const ScanStepArgs* a, hipStream_t stream);
 size_t amp_delta_blocks(size_t rows, size_t n);
-size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t dk, size_t dv, int backward);
+size_t amp_delta_workspace_bytes(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk, size_t dv, int backward);
 hipError_t amp_delta_forward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
 hipError_t amp_delta_backward_launch(int dtype, const DeltaArgs* a, hipStream_t stream);
 hipError_t amp_delta_step_launch(int dtype, const DeltaStepArgs* a, hipStream_t stream);
