@@ -153,6 +153,12 @@ __device__ __forceinline__ void parts4(const Vec<T, 4>& v, v2u (&u)[P]) {
   split4<P>(x, u);
 }
 
+// base + bytes, for a base that is the same for all lanes.
+template <class T>
+__device__ __forceinline__ const T* past(const T* base, unsigned bytes) { return (const T*)((const char*)base + bytes); }
+template <class T>
+__device__ __forceinline__ T* past(T* base, unsigned bytes) { return (T*)((char*)base + bytes); }
+
 // Four elements, n and later replaced by zeros. `fours`, the same for all lanes: n is a multiple of 4, as where dk and dv are. (A branch for
 // every count of elements instead costs the kernels' loops registers, which they spill.) p can be read where n is 0 as well.
 template <class T>
@@ -367,11 +373,23 @@ __global__ __launch_bounds__(256) void delta_zero_kernel(DeltaArgs a) {
 }
 
 // ------------------------------------------------------------------ per block and head: N, P and the sums of decays
+// e^x of a difference of sums: half a step of its exponent and the instruction's own.
+__device__ __forceinline__ float power(double x) { return __builtin_amdgcn_exp2f((float)(x * 1.4426950408889634)); }
+
+// N = (1 + M beta)^-1 M of a chunk in halves of 16 rows: those on the diagonal row after row, N = M - (M beta) N, a lane to a column; the one
+// below them from two products, N21 = W - N22 beta W with W = M21 - M21 beta N11.
 template <class T, int KT>
 __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
-  constexpr int P = In<T>::P;
-  __shared__ Matrix<P, B, KT * 32> k, q;
-  __shared__ float mat[2][2][C][C + 4];   // chunk, K K^T or Q K^T
+  constexpr int P = In<T>::P, LM = C + 4;
+  __shared__ union {
+    struct {
+      Matrix<P, B, KT * 32> k, q;
+    } in;
+    struct {
+      alignas(16) float mat[2][2][C][LM];   // chunk; M beta (first K K^T), M (first Q K^T)
+      float n[4][16][17];                   // the halves on the diagonal
+    } m;
+  } u;
   __shared__ double g[B];
   __shared__ float beta[B];
   const int h = blockIdx.x % a.heads, hk = h / (a.heads / a.key_heads);
@@ -379,18 +397,15 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
   if (!find_block(a, blockIdx.x / a.heads, w)) return;
   const T* K = row_of((const T*)a.k, w.row, a.k_stride) + (size_t)hk * a.dk;
   const T* Q = row_of((const T*)a.q, w.row, a.q_stride) + (size_t)hk * a.dk;
-  constexpr int UNITS = B * KT * 8;
-#pragma unroll
-  for (int j = 0; j < UNITS / 256; ++j) {
-    const int u = threadIdx.x + j * 256, row = u / (KT * 8), four = u % (KT * 8);
-    const long n = row < w.count ? a.dk - four * 4 : 0;
-    v2u x[P];
-    parts4(load_four(K + (row < w.count ? row : 0) * a.k_stride + (n > 0 ? four * 4 : 0), n, a.fours), x);
-    k.put(row, four, x);
-    parts4(load_four(Q + (row < w.count ? row : 0) * a.q_stride + (n > 0 ? four * 4 : 0), n, a.fours), x);
-    q.put(row, four, x);
-  }
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  constexpr int PER = B * KT * 8 / 256;
+  Vec<T, 4> kv[PER], qv[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int x = threadIdx.x + j * 256, row = x / (KT * 8), four = x % (KT * 8), n = row < w.count ? a.dk - four * 4 : 0;
+    kv[j] = load_four(past(K, n > 0 ? (row * (unsigned)a.k_stride + four * 4) * (unsigned)sizeof(T) : 0u), n, a.fours);
+    qv[j] = load_four(past(Q, n > 0 ? (row * (unsigned)a.q_stride + four * 4) * (unsigned)sizeof(T) : 0u), n, a.fours);
+  }
   if (wave == 0) {
     float d = 0.f, bt = 0.f;
     if (lane < w.count) {
@@ -409,63 +424,97 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs a) {
     sums_of(a, w.index, h)[lane] = sum;
     const double end = __shfl(sum, C - 1, C);
     float* f = scalars_of(a, w.index, h);
-    f[lane] = expf((float)sum);
-    f[B + lane] = expf((float)(end - sum));
+    f[lane] = power(sum);
+    f[B + lane] = power(end - sum);
     f[2 * B + lane] = bt;
-    if (lane % C == 0) f[3 * B + lane / C] = expf((float)end);
+    if (lane % C == 0) f[3 * B + lane / C] = power(end);
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int x = threadIdx.x + j * 256;
+    v2u y[P];
+    parts4(kv[j], y);
+    u.in.k.put(x / (KT * 8), x % (KT * 8), y);
+    parts4(qv[j], y);
+    u.in.q.put(x / (KT * 8), x % (KT * 8), y);
   }
   __syncthreads();
+  const int c16 = lane % 16, q = lane / 16;
+  v4f acc[3] = {};
   {   // a wave to each product of each chunk: its three tiles that have elements on or below the diagonal
-    const int chunk = wave / 2, r0 = chunk * C, c = lane % 16;
-    const Matrix<P, B, KT * 32>& left = wave % 2 ? q : k;
-    v4f acc[3] = {};
+    const int r0 = wave / 2 * C;
+    const Matrix<P, B, KT * 32>& left = wave % 2 ? u.in.q : u.in.k;
 #pragma unroll
     for (int f = 0; f < KT; ++f) {
       const Frag<P> a0 = left.along(r0, f), a1 = left.along(r0 + 16, f);
-      const Frag<P> b0 = k.along(r0, f), b1 = k.along(r0 + 16, f);
+      const Frag<P> b0 = u.in.k.along(r0, f), b1 = u.in.k.along(r0 + 16, f);
       acc[0] = mma<3>(a0, b0, acc[0]);
       acc[1] = mma<3>(a1, b0, acc[1]);
       acc[2] = mma<3>(a1, b1, acc[2]);
     }
+  }
+  __syncthreads();
+  // the decays, by the lanes that hold the products: P is finished, M and M beta go on
+  {
+    const int chunk = wave / 2;
+    float* out = matrices_of(a, w.index, h, chunk) + C * C;
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mat[chunk][wave % 2][(t ? 16 : 0) + 4 * (lane / 16) + i][(t == 2 ? 16 : 0) + c] = acc[t][i];
-  }
-  __syncthreads();
-  // the decays: P is finished, M beta takes M's place
+      for (int i = 0; i < 4; ++i) {
+        const int r = (t ? 16 : 0) + 4 * q + i, c = (t == 2 ? 16 : 0) + c16;
+        const float x = power(g[chunk * C + r] - g[chunk * C + c]) * acc[t][i];
+        if (wave % 2) {
+          out[r * C + c] = r >= c ? a.scale * x : 0.f;
+        } else {
+          const float m = r > c ? x : 0.f;
+          u.m.mat[chunk][1][r][c] = m;
+          u.m.mat[chunk][0][r][c] = m * beta[chunk * C + c];
+        }
+      }
+    if (wave % 2)
 #pragma unroll
-  for (int j = 0; j < 2 * C * C / 256; ++j) {
-    const int e = threadIdx.x + j * 256, chunk = e / (C * C), r = e / C % C, c = e % C;
-    const float d = r >= c ? expf((float)(g[chunk * C + r] - g[chunk * C + c])) : 0.f;
-    matrices_of(a, w.index, h, chunk)[C * C + r * C + c] = r >= c ? a.scale * d * mat[chunk][1][r][c] : 0.f;
-    mat[chunk][1][r][c] = r > c ? d * mat[chunk][0][r][c] : 0.f;
-    mat[chunk][0][r][c] = r > c ? d * mat[chunk][0][r][c] * beta[chunk * C + c] : 0.f;
+      for (int i = 0; i < 4; ++i) out[(4 * q + i) * C + 16 + c16] = 0.f;
   }
   __syncthreads();
-  // N = M - (M beta) N, row after row, a lane to a column
   if (wave == 0) {
-    const int chunk = lane / C, c = lane % C;
-    float n[C];
+    const int chunk = q / 2, o = q % 2 * 16;
+    float n[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float s[4] = {u.m.mat[chunk][1][o + r][o + c16], 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int m = 0; m < r; ++m) s[m % 4] = fmaf(-u.m.mat[chunk][0][o + r][o + m], n[m], s[m % 4]);
+      n[r] = (s[0] + s[1]) + (s[2] + s[3]);
+      u.m.n[q][r][c16] = n[r];
+    }
     float* out = matrices_of(a, w.index, h, chunk);
 #pragma unroll
-    for (int r = 0; r < C; ++r) {
-      float s[4] = {mat[chunk][1][r][c], 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int m = 0; m < r; ++m) s[m % 4] = fmaf(-mat[chunk][0][r][m], n[m], s[m % 4]);
-      n[r] = (s[0] + s[1]) + (s[2] + s[3]);
-      out[r * C + c] = n[r];
+    for (int r = 0; r < 16; ++r) {
+      out[(o + r) * C + o + c16] = n[r];
+      if (o == 0) out[r * C + 16 + c16] = 0.f;
     }
+  }
+  __syncthreads();
+  if (wave < 2) {   // a chunk to each; a result's rows 4 q + i are the next product's contracted index, in that order
+    const int chunk = wave;
+    v4f x, y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = u.m.mat[chunk][1][16 + 4 * q + i][c16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x = __builtin_amdgcn_mfma_f32_16x16x4f32(-u.m.mat[chunk][0][16 + c16][4 * q + i], u.m.n[2 * chunk][4 * q + i][c16], x, 0, 0, 0);
+    y = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      y = __builtin_amdgcn_mfma_f32_16x16x4f32(-u.m.n[2 * chunk + 1][c16][4 * q + i] * beta[chunk * C + 16 + 4 * q + i], x[i], y, 0, 0, 0);
+    float* out = matrices_of(a, w.index, h, chunk);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[(16 + 4 * q + i) * C + c16] = y[i];
   }
 }
 
 // ------------------------------------------------------------------ the chain over a sequence's chunks
-// base + bytes, for a base that is the same for all lanes.
-template <class T>
-__device__ __forceinline__ const T* past(const T* base, unsigned bytes) { return (const T*)((const char*)base + bytes); }
-template <class T>
-__device__ __forceinline__ T* past(T* base, unsigned bytes) { return (T*)((char*)base + bytes); }
-
 // What a chunk's waves share, on its way from memory and in LDS. OUT: with Q and P (in PN parts), else K and N alone.
 template <class T, int KT, int W, int PN, bool OUT>
 struct Chunk {
@@ -893,38 +942,54 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
 }
 
 // From segment to segment: the state in front of the next (backward: the gradient behind the one before) is the map's share of this one's and what
-// the segment leaves of no state, which lies there already.
-template <int KT, int W, bool BACK>
-__global__ __launch_bounds__(64 * W) void delta_join_kernel(DeltaArgs a) {
-  const int h = blockIdx.x % a.heads, c16 = threadIdx.x % 16, q = threadIdx.x % 64 / 16;
+// the segment leaves of no state, which lies there already. 64 columns to a workgroup, whose waves share a map's parts in LDS; the next
+// map is on its way meanwhile.
+template <int KT, bool BACK>
+__global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
+  constexpr int PER = 32 * KT * KT * 8 / 256;
+  __shared__ Matrix<3, 32 * KT, 32 * KT> map;
+  const int h = blockIdx.x % a.heads;
   const size_t s = blockIdx.x / a.heads;
   const long size = a.begin ? a.first_segment[a.n_seq + 1] : a.segment, blocks = first_block(a, s + 1) - first_block(a, s);
   const long count = blocks > size ? (blocks + size - 1) / size : 1;
   if (count < 3) return;
-  const Columns m(a, W, false);
-  if (!m.any) return;
+  const int col = (blockIdx.y * 4 + threadIdx.x / 64) * 16 + threadIdx.x % 16;
   const size_t base = first_segment(a, s);
+  const auto place = [&](long j) { return base + (BACK ? count - 1 - j : j); };
+  Vec<float, 4> next[PER];
+  const auto fetch = [&](long j) {
+    const float* p = map_of(a, place(j), h);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int x = threadIdx.x + i * 256, row = x / (KT * 8), four = x % (KT * 8), n = row < a.dk ? a.dk - 4 * four : 0;
+      next[i] = load_four(past(p, n > 0 ? (unsigned)(row * a.dk + 4 * four) * 4u : 0u), n, a.fours);
+    }
+  };
+  fetch(1);
   State<KT> S;
-  S.load(front_of(a, base + (BACK ? count - 2 : 1), h), a.dk, a.dv, m.col);
+  S.load(front_of(a, place(1), h), a.dk, a.dv, col);
   for (long j = 1; j + 1 < count; ++j) {
-    const size_t at = base + (BACK ? count - 1 - j : j), to = BACK ? at - 1 : at + 1;
-    const float* map = map_of(a, at, h);
-    State<KT> next;
-    next.load(front_of(a, to, h), a.dk, a.dv, m.col);
+    float* to = front_of(a, place(j + 1), h);
+    State<KT> sum;
+    sum.load(to, a.dk, a.dv, col);
+    __syncthreads();   // the map in front is done with
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int x = threadIdx.x + i * 256;
+      v2u y[3];
+      parts4(next[i], y);
+      map.put(x / (KT * 8), x % (KT * 8), y);
+    }
+    __syncthreads();
+    if (j + 2 < count) fetch(j + 1);
 #pragma unroll
     for (int f = 0; f < KT; ++f) {
       const Frag<3> op = S.operand(f);
 #pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) {
-        const int r = 16 * i + c16, k0 = 32 * f + 4 * q;
-        const Vec<float, 4> lo = load_four(map + (r < a.dk && k0 < a.dk ? r * a.dk + k0 : 0), r < a.dk ? a.dk - k0 : 0, a.fours);
-        const Vec<float, 4> hi = load_four(map + (r < a.dk && k0 + 16 < a.dk ? r * a.dk + k0 + 16 : 0), r < a.dk ? a.dk - k0 - 16 : 0, a.fours);
-        const float x[8] = {get(lo, 0), get(lo, 1), get(lo, 2), get(lo, 3), get(hi, 0), get(hi, 1), get(hi, 2), get(hi, 3)};
-        next.t[i] = mma<3>(split8<3>(x), op, next.t[i]);
-      }
+      for (int i = 0; i < 2 * KT; ++i) sum.t[i] = mma<3>(map.along(16 * i, f), op, sum.t[i]);
     }
-    next.store(front_of(a, to, h), a.dk, a.dv, m.col);
-    S = next;
+    sum.store(to, a.dk, a.dv, col);
+    S = sum;
   }
 }
 
@@ -1437,7 +1502,7 @@ hipError_t chain(const DeltaArgs& a, hipStream_t stream) {
     if constexpr (BACK) e = launch(delta_backward_kernel<T, KT, W, false>, dim3(x, groups(values + keys)), dim3(64 * W), 0, stream, a);
     else e = launch(delta_forward_kernel<T, KT, W, false>, dim3(x, groups(values + keys)), dim3(64 * W), 0, stream, a);
     if (e == hipSuccess)
-      e = launch(delta_join_kernel<KT, W, BACK>, dim3((unsigned)(a.n_seq * a.heads), groups(values)), dim3(64 * W), 0, stream, a);
+      e = launch(delta_join_kernel<KT, BACK>, dim3((unsigned)(a.n_seq * a.heads), (a.dv + 63) / 64), dim3(256), 0, stream, a);
   }
   if (e != hipSuccess) return e;
   if constexpr (BACK) return launch(delta_backward_kernel<T, KT, W, true>, dim3(x, groups(values)), dim3(64 * W), 0, stream, a);
