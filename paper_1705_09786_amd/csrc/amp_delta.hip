@@ -98,6 +98,18 @@ __device__ __forceinline__ void mma2(const Frag<PA> (&a)[2], const Frag<PB>& b, 
           c[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a[r].p[i]), __builtin_bit_cast(v8bf, b.p[s - i]), c[r], 0, 0, 0);
 }
 
+// The sum over a lane's 16 (8), by rotations within them: lane 0's is added up in the same order always.
+template <int W>
+__device__ __forceinline__ float rotate(float v) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + W, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum16(float v) {
+  v += rotate<8>(v);
+  v += rotate<4>(v);
+  v += rotate<2>(v);
+  return v + rotate<1>(v);
+}
+
 // Matrices in LDS. An operand is read along its rows, 8 bytes from each of 16 rows at a time, or down its columns, transposed, 32 bytes from each of
 // four rows: rows 8 words more than a multiple of 32 apart, and 2 between fours of them, put either's 16 lanes on 32 banks of their own.
 template <int P, int ROWS, int COLS>
@@ -135,8 +147,12 @@ struct Matrix {
   }
 };
 
-// Nothing moves across: the reads in front are on their way while what follows is worked on.
-__device__ __forceinline__ void on_their_way() { __builtin_amdgcn_sched_barrier(0); }
+// Nothing moves across: the reads in front are on their way while what follows is worked on. (Not where four waves share a SIMD: they have
+// half the registers, and one another to wait with.)
+template <bool PIN>
+__device__ __forceinline__ void on_their_way() {
+  if constexpr (PIN) __builtin_amdgcn_sched_barrier(0);
+}
 
 template <int P>
 __device__ __forceinline__ void split4(const float (&x)[4], v2u (&u)[P]) {
@@ -270,6 +286,7 @@ struct Job {
 // Segment `index` of all of them.
 __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& w) {
   if (!a.segments) {
+    if (a.begin && a.n_seq <= DELTA_ORDER) index = a.order[index];
     w.s = index, w.from = 0, w.to = first_block(a, index + 1) - first_block(a, index), w.first = w.last = true;
     return index < a.n_seq;
   }
@@ -278,6 +295,7 @@ __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& 
   if (a.begin) {
     size = a.first_segment[a.n_seq + 1];
     if ((long)index >= a.first_segment[hi]) return false;
+    if (a.n_seq <= DELTA_ORDER && a.first_segment[hi] == (int)hi) index = a.order[index];   // no sequence is cut
     while (hi - lo > 1) {
       const size_t mid = (lo + hi) / 2;
       (a.first_segment[mid] <= (long)index ? lo : hi) = mid;
@@ -330,6 +348,15 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
     Block w;
     const bool in = search_block(a, i, w);
     a.table[2 * i] = in ? (int)w.row : 0, a.table[2 * i + 1] = in ? w.count : 0;
+  }
+  if (a.n_seq <= DELTA_ORDER && threadIdx.x < a.n_seq) {   // the longest sequences first: 24 of up to 1,350 rows on 16 heads 230 us for 300
+    const int mine = a.first[threadIdx.x + 1] - a.first[threadIdx.x];
+    int front = 0;
+    for (int s = 0; s < (int)a.n_seq; ++s) {
+      const int other = a.first[s + 1] - a.first[s];
+      front += other > mine || (other == mine && s < (int)threadIdx.x);
+    }
+    a.order[front] = (int)threadIdx.x;
   }
   if (!a.segments) return;
   for (int d = 1; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d, 64));
@@ -672,7 +699,7 @@ __device__ __forceinline__ float* map_of(const DeltaArgs& a, size_t segment, int
 
 // OUT: the chain with its outputs, from the states in front of the segments; else the segments' maps, and what they leave of no state.
 template <class T, int KT, int W, bool OUT>
-__global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(DeltaArgs a) {
   constexpr int PO = sizeof(T) == 2 ? 2 : 3;   // o is rounded to 16 bits: two parts leave 2^-16 of its terms
   typedef Chunk<T, KT, W, PO, OUT> Ck;
   __shared__ typename Ck::Shared sh[2];
@@ -713,10 +740,12 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
     const typename Ck::Shared& t = sh[c & 1];
     const long row = b + (long)c * C;
     const int count = rows_in(c);
-    if (c + 1 < chunks) fetch(c + 1);
+    if (OUT && c + 1 < chunks) fetch(c + 1);
+    v4f oq[2] = {};
+    float x[8], y[8];
     if (m.any) {
       if (OUT && a.carry && c % 2 == 0) S.store(a.carry + a.carry_states + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
-      v4f ks[2] = {}, oq[2] = {};
+      v4f ks[2] = {};
       Frag<In<T>::P> kf[2][2], qf[2][2];
       const auto read = [&](int f) {
 #pragma unroll
@@ -726,7 +755,7 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
         }
       };
       read(0);
-      const Eight grow(t.grow), beta(t.beta), rest(t.rest);
+      const Eight grow(t.grow), beta(t.beta);
       const float whole = t.whole;
       Frag<3> nf[2];
 #pragma unroll
@@ -735,7 +764,7 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
         else
 #pragma unroll
           for (int r = 0; r < 2; ++r) nf[r] = t.n.along(16 * r, 0);
-        on_their_way();
+        on_their_way<OUT>();
         const v4f decayed[2] = {S.t[2 * f] * whole, S.t[2 * f + 1] * whole};
         const Frag<3> op = S.operand(f);
         S.t[2 * f] = decayed[0], S.t[2 * f + 1] = decayed[1];
@@ -744,17 +773,10 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) oq[r] = mma<PO>(op, qf[f % 2][r], oq[r]);
       }
-      Frag<In<T>::P> kd[2];
-      kd[0] = t.k.down(0, 0);
-      Frag<PO> pf[2];
-      if constexpr (OUT)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) pf[r] = t.p.along(16 * r, 0);
-      on_their_way();
-      float x[8], y[8];
+      on_their_way<OUT>();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        x[k] = (m.map ? 0.f : widen(v.v[k])) - grow[k] * ks[k / 4][k % 4];
+        x[k] = (m.map ? 0.f : widen((OUT ? v : vnext).v[k])) - grow[k] * ks[k / 4][k % 4];
         y[k] = beta[k] * x[k];
       }
       const Frag<3> rb = split8<3>(y);
@@ -762,6 +784,10 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
       mma2<3>(nf, rb, nr);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] -= nr[k / 4][k % 4];
+    }
+    if (!OUT && c + 1 < chunks) fetch(c + 1);
+    if (m.any) {
+      const Eight beta(t.beta), rest(t.rest);
       if (OUT && a.carry && col < a.dv) {
         const size_t wide = (size_t)a.heads * a.dv;
         float* E = a.carry + row * wide + (size_t)h * a.dv;
@@ -775,15 +801,11 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
         x[k] *= beta[k];
         y[k] = rest[k] * x[k];
       }
-      const Frag<3> up = split8<3>(y);
-#pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) {
-        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0);
-        on_their_way();
-        S.t[i] = mma<3>(kd[i % 2], up, S.t[i]);
-      }
       if constexpr (OUT) {
         if (a.o) {
+          Frag<PO> pf[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) pf[r] = t.p.along(16 * r, 0);
           const Frag<PO> vo = split8<PO>(x);
           T* O = (T*)a.o + row * a.o_stride + (size_t)h * a.dv + m.c0;
 #pragma unroll
@@ -796,11 +818,18 @@ __global__ __launch_bounds__(64 * W) void delta_forward_kernel(DeltaArgs a) {
           }
         }
       }
+      Frag<In<T>::P> kd[2];
+      kd[0] = t.k.down(0, 0);
+      const Frag<3> up = split8<3>(y);
+#pragma unroll
+      for (int i = 0; i < 2 * KT; ++i) {
+        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0);
+        on_their_way<OUT>();
+        S.t[i] = mma<3>(kd[i % 2], up, S.t[i]);
+      }
     }
-    if (c + 1 < chunks) {
-      next.put(sh[(c + 1) & 1]);
-      v = vnext;
-    }
+    if (c + 1 < chunks) next.put(sh[(c + 1) & 1]);
+    if (OUT) v = vnext;
     __syncthreads();
   }
   if (OUT) {
@@ -856,7 +885,9 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     const typename Ck::Shared& t = sh[c & 1];
     const long row = b + (long)c * C;
     const int count = rows_in(c);
-    if (c > 0) fetch(c - 1);
+    if (OUT && c > 0) fetch(c - 1);
+    float x[8], y[8];
+    Frag<3> od;
     if (m.any) {
       if (OUT && (c % 2 || c == chunks - 1)) S.store(a.behind + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
       v4f ks[2] = {};
@@ -875,7 +906,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
         else
 #pragma unroll
           for (int r = 0; r < 2; ++r) pf[r] = t.p.down(r, 0);
-        on_their_way();
+        on_their_way<OUT>();
         const v4f decayed[2] = {S.t[2 * f] * whole, S.t[2 * f + 1] * whole};
         const Frag<3> op = S.operand(f);
         S.t[2 * f] = decayed[0], S.t[2 * f + 1] = decayed[1];
@@ -883,21 +914,17 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       }
 #pragma unroll
       for (int r = 0; r < 2; ++r) nf[r] = t.n.down(r, 0);
-      on_their_way();
-      float x[8], y[8];
+      on_their_way<OUT>();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = m.map ? 0.f : widen(d.v[k]);
+      for (int k = 0; k < 8; ++k) x[k] = m.map ? 0.f : widen((OUT ? d : dnext).v[k]);
       const Frag<P> dop = split8<P>(x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         ks[k / 4][k % 4] *= rest[k];
         y[k] = a.scale * grow[k] * x[k];
       }
-      const Frag<3> od = split8<3>(y);
+      od = split8<3>(y);
       mma2<3>(pf, dop, ks);
-      Frag<P> kd[2], qd[2];
-      kd[0] = t.k.down(0, 0), qd[0] = t.q.down(0, 0);
-      on_their_way();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         x[k] = ks[k / 4][k % 4];
@@ -908,6 +935,13 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       mma2<3>(nf, z, nz);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] -= nz[k / 4][k % 4];
+    }
+    if (!OUT && c > 0) fetch(c - 1);
+    if (m.any) {
+      const Eight grow(t.grow), beta(t.beta);
+      Frag<P> kd[2], qd[2];
+      kd[0] = t.k.down(0, 0), qd[0] = t.q.down(0, 0);
+      on_their_way<OUT>();
       if (OUT && col < a.dv) {
         const size_t wide = (size_t)a.heads * a.dv;
         float* X = a.x + row * wide + (size_t)h * a.dv;
@@ -922,14 +956,12 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
 #pragma unroll
       for (int i = 0; i < 2 * KT; ++i) {
         if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0), qd[(i + 1) % 2] = t.q.down(i + 1, 0);
-        on_their_way();
+        on_their_way<OUT>();
         S.t[i] = mma<3>(kd[i % 2], down, mma<3>(qd[i % 2], od, S.t[i]));
       }
     }
-    if (c > 0) {
-      next.put(sh[(c - 1) & 1]);
-      d = dnext;
-    }
+    if (c > 0) next.put(sh[(c - 1) & 1]);
+    if (OUT) d = dnext;
     __syncthreads();
   }
   if (OUT) {
@@ -1235,7 +1267,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
         if (owner)
 #pragma unroll
           for (int z = P - 1; z >= 0; --z) x += widen(kq.at[z][kq.place(r, kc)]);
-        x = group_sum<16>(x * dq[t][i]);
+        x = sum16(x * dq[t][i]);
         if (c16 == 0) u.rows.dots[wave][r] = x;
       }
     tail = group_sum<64>(tail);
@@ -1253,7 +1285,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
         const bool there = t >= 10 ? r > j : r >= j;
         pair[k][i] = there ? (t >= 10 ? -1.f : a.scale) * expf((float)(g[r] - g[j])) * pair[k][i] : 0.f;
         if (t < 10) {
-          const float y = group_sum<16>(pair[k][i] * qk[k < 2 ? k : 0][i]);
+          const float y = sum16(pair[k][i] * qk[k < 2 ? k : 0][i]);
           if (c16 == 0) u.rows.prow[jt][r] = y;
         }
       }
@@ -1421,7 +1453,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
 
 // ------------------------------------------------------------------ launches
 struct Sizes {
-  size_t blocks, segments, first, first_segment, table, matrices, scalars, sums, x, behind, kept, fronts, maps, bytes;   // offsets into the workspace
+  size_t blocks, segments, first, first_segment, order, table, matrices, scalars, sums, x, behind, kept, fronts, maps, bytes;   // offsets into the workspace
 };
 Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk, size_t dv, bool backward) {
   Sizes s;
@@ -1435,6 +1467,7 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk,
   };
   s.first = take((n + 1) * sizeof(int));
   s.first_segment = take((n + 2) * sizeof(int));
+  s.order = take(n <= DELTA_ORDER ? n * sizeof(int) : 0);
   s.table = take(s.blocks * 2 * sizeof(int));
   s.matrices = take(s.blocks * heads * 4 * C * C * sizeof(float));
   s.scalars = take(s.blocks * heads * 4 * B * sizeof(float));
@@ -1459,6 +1492,7 @@ void lay_out(DeltaArgs& a, bool backward) {
   a.segments = s.segments;
   a.first = (int*)(w + s.first);
   a.first_segment = (int*)(w + s.first_segment);
+  a.order = (int*)(w + s.order);
   a.table = (int*)(w + s.table);
   a.matrices = (float*)(w + s.matrices);
   a.scalars = (float*)(w + s.scalars);

@@ -61,6 +61,7 @@ struct DistillArgs {
 #define DELTA_CHUNK 32   // rows whose errors are solved for together
 #define DELTA_BLOCK 64   // rows between two states that the backward pass starts from
 #define DELTA_SEGMENT 8  // blocks of the shortest segments that a long sequence is cut into
+#define DELTA_ORDER 256  // sequences that are put in order, the longest first
 #define DELTA_MAX_KEY 128
 
 struct DeltaZero {   // an output whose rows of no sequence become zeros: bytes between rows, 16-bit halves of a row
@@ -90,7 +91,7 @@ struct DeltaArgs {
   int fours;
   size_t blocks, carry_states, segments;   // segments: at most, 0 = sequences stay whole
   long segment;                            // blocks of one, where there is no plan
-  int *first, *first_segment, *table;
+  int *first, *first_segment, *order, *table;
   float *matrices, *scalars, *x, *behind, *kept, *fronts, *maps;
   double* sums;
 };
