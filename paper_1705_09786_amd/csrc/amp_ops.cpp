@@ -210,6 +210,23 @@ struct Range {
 
 // No result overlaps anything but its own tensor, and that only as a whole.
 int check_results(const char* what, size_t n, const amp_tensor* t, const float* norm, const void* ws, size_t need) {
+  // as most lists are: the results one behind the other in a buffer of their own, none of the tensors in it
+  uintptr_t from = UINTPTR_MAX, to = 0;
+  bool plain = true;
+  const auto outside = [&](const void* p, size_t bytes) { return !p || !bytes || (uintptr_t)p >= to || (uintptr_t)p + bytes <= from; };
+  for (size_t i = 0; i < n && plain; ++i)
+    if (t[i].n && t[i].out) {
+      plain = t[i].out != t[i].p && (uintptr_t)t[i].out >= to;
+      from = std::min(from, (uintptr_t)t[i].out), to = (uintptr_t)t[i].out + t[i].n * elem(t[i].dtype);
+    }
+  for (size_t i = 0; i < n && plain; ++i) {
+    const size_t bytes = t[i].n * elem(t[i].dtype);
+    plain = outside(t[i].p, bytes) && ((uintptr_t)norm >= (uintptr_t)t[i].p + bytes || (uintptr_t)norm + sizeof(float) <= (uintptr_t)t[i].p) &&
+            ((uintptr_t)ws >= (uintptr_t)t[i].p + bytes || (uintptr_t)ws + need <= (uintptr_t)t[i].p);
+  }
+  if (plain && outside(norm, sizeof(float)) && outside(ws, need) &&
+      ((uintptr_t)norm >= (uintptr_t)ws + need || (uintptr_t)norm + sizeof(float) <= (uintptr_t)ws))
+    return AMP_OK;
   Range* r = (Range*)malloc((2 * n + 2) * sizeof(Range));
   if (!r) return fail(AMP_ENOMEM, "%s: no host memory for %zu ranges", what, 2 * n + 2);
   size_t m = 0;

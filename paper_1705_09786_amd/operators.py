@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes as ct
 from array import array
 from functools import lru_cache
+from operator import attrgetter
 
 import torch
 
@@ -453,34 +454,57 @@ def token_logprob(logits, index, temperature=1.0):
 
 
 # ------------------------------------------------------------------ norm and clipping
+# A list of hundreds of tensors is looked at attribute by attribute, each for all of them without a line of Python (50 us for 600 of them).
+_type, _needs_grad = attrgetter("dtype"), attrgetter("requires_grad")
+_address, _elements, _device, _packed = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
+
+
+def _many(name, tensors, device):
+    """(their types, their device) of tensors that a call over many takes."""
+    if not all(isinstance(t, torch.Tensor) for t in tensors):
+        _refuse("%s: one is not a tensor" % name)
+    types, devices = set(map(_type, tensors)), set(map(_device, tensors))
+    if not types <= DTYPES.keys() or len(devices) > 1 or -1 in devices or not all(map(_packed, tensors)) or \
+            (device is not None and devices != {device}):
+        _refuse("%s: one is not a contiguous tensor of a float type on the GPU of the first" % name)
+    if torch.is_grad_enabled() and any(map(_needs_grad, tensors)):
+        _differentiated("one of %s" % name)
+    return types, devices.pop() if devices else device
+
+
 def clip_gradients(gradients, max_norm=None, *, out=None):
     """The norm of all elements of the tensors together, a float32 tensor without dimensions; with max_norm the tensors are multiplied by
-    min(1, max_norm / norm), in place or into the tensors of `out` (of the same shapes and types).  gradients: contiguous tensors of any
+    min(1, max_norm / norm), in place or into the tensors of `out` (of the same sizes and types).  gradients: contiguous tensors of any
     shapes on one GPU, float32, bfloat16 or float16.  A norm that is not finite leaves them as they are."""
     gradients = list(gradients)
     if not gradients:
         _refuse("there are no gradients")
     if out is not None and max_norm is None:
         _refuse("out without max_norm")
-    results = None if max_norm is None else gradients if out is None else list(out)
-    first = gradients[0]
-    grad_mode, device = torch.is_grad_enabled(), first.get_device() if isinstance(first, torch.Tensor) else -1
-    for name, tensors in (("gradients", gradients),) + ((("out", results),) if out is not None else ()):
-        for i, t in enumerate(tensors):
-            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in DTYPES or t.get_device() != device or not t.is_contiguous():
-                _refuse("%s[%d] is not a contiguous tensor of a float type on the GPU of the first" % (name, i))
-            if grad_mode and t.requires_grad:
-                _differentiated("%s[%d]" % (name, i))
-    if out is not None and ([t.shape for t in results] != [t.shape for t in gradients] or [t.dtype for t in results] != [t.dtype for t in gradients]):
-        _refuse("out has other shapes or types than the gradients")
-    p = [t.data_ptr() for t in gradients]
-    to = [0] * len(p) if results is None else p if out is None else [t.data_ptr() for t in results]
-    table = array("Q", [x for item in zip(p, to, [t.numel() for t in gradients], [DTYPES[t.dtype] for t in gradients]) for x in item])
+    types, device = _many("gradients", gradients, None)
+    p, sizes, to = list(map(_address, gradients)), list(map(_elements, gradients)), 0
+    if max_norm is not None:
+        to = p
+    if out is not None:
+        out = list(out)
+        other = _many("out", out, device)[0]
+        if len(out) != len(gradients) or list(map(_elements, out)) != sizes or (
+                (len(types) > 1 or other != types) and [t.dtype for t in out] != [t.dtype for t in gradients]):
+            _refuse("out has other sizes or types than the gradients")
+        to = list(map(_address, out))
+    n, first = len(p), gradients[0]
+    table = array("Q", bytes(32 * n))   # amp_tensor: p, out, n, dtype
+    table[0::4], table[2::4] = array("Q", p), array("Q", sizes)
+    if to:
+        table[1::4] = array("Q", to)
+    one = DTYPES[first.dtype]
+    if len(types) > 1 or one:
+        table[3::4] = array("Q", [DTYPES[t.dtype] for t in gradients] if len(types) > 1 else [one] * n)
     at, nb = table.buffer_info()[0], ct.c_size_t()
-    _check(B.lib().amp_clip_workspace(len(p), at, ct.byref(nb)))
+    _check(B.lib().amp_clip_workspace(n, at, ct.byref(nb)))
     norm = torch.empty((), dtype=torch.float32, device=first.device)
     ws = torch.empty(nb.value, dtype=torch.uint8, device=first.device)
-    _call(first, "amp_clip_gradients", len(p), at, float("inf") if max_norm is None else max_norm, norm.data_ptr(), ws.data_ptr(), nb.value)
-    if results is not None:
-        _written(tuple(results))
+    _call(first, "amp_clip_gradients", n, at, float("inf") if max_norm is None else max_norm, norm.data_ptr(), ws.data_ptr(), nb.value)
+    if max_norm is not None:
+        _written(tuple(gradients if out is None else out))
     return norm

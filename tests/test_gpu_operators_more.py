@@ -559,7 +559,9 @@ def test_refusals_on_tensors():
     refused("contiguous", ops.clip_gradients, [g[0].double()])
     refused("max_norm", ops.clip_gradients, g, -1.0)
     refused("out", ops.clip_gradients, g, out=g)
-    refused("shapes", ops.clip_gradients, g, 1.0, out=g[:1])
+    refused("sizes", ops.clip_gradients, g, 1.0, out=g[:1])
+    refused("types", ops.clip_gradients, g, 1.0, out=[torch.ones_like(t, dtype=torch.half) for t in g])
+    refused("not a tensor", ops.clip_gradients, [g[0], 1.0])
     refused("overlaps", ops.clip_gradients, [g[0], g[0]], 1.0)
     refused("overlaps", ops.clip_gradients, [g[0][:3], g[0][2:]], 1.0)
     refused("requires grad", ops.clip_gradients, [g[0].clone().requires_grad_()])
