@@ -150,9 +150,9 @@ __global__ __launch_bounds__(TPB) void policy_kernel(PolicyArgs a) {
 }
 
 // Rows under a running maximum: without a gradient, or (GRADIENT) read again for it where registers do not hold them.
-template <class T, bool GRADIENT>
-__global__ __launch_bounds__(1024) void policy_stream_kernel(PolicyArgs a) {
-  constexpr int TPB = 1024, N = Vec<T>::N, NW = TPB / 64, DEEP = 4;
+template <class T, int TPB, bool GRADIENT>
+__global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
+  constexpr int N = Vec<T>::N, NW = TPB / 64, DEEP = 4;
   __shared__ float top[NW];
   __shared__ double part[NW];
   __shared__ Row row;
@@ -166,27 +166,42 @@ __global__ __launch_bounds__(1024) void policy_stream_kernel(PolicyArgs a) {
   if ((w == 0.f && !a.logprob) || own < 0) return left_out<TPB, T>(a, r, dx, true);
   const float mine = widen(x[own]);
   float m = -INFINITY, s = 0.f;
-  for (long c0 = threadIdx.x * N; c0 < classes; c0 += DEEP * TPB * N) {
-    Vec<T> v[DEEP];
-#pragma unroll
-    for (int j = 0; j < DEEP; ++j) {
-      const long c = c0 + (long)j * TPB * N;
-      if (c < classes) v[j] = load_vec(x + c, classes - c);
-    }
+  // DEEP groups to the running maximum and its sum; of terms that are all 0 so far (a maximum of -infinity) nothing is left to rescale
+  const auto add = [&](const Vec<T>(&v)[DEEP], auto in) {
     float most = m;
 #pragma unroll
     for (int j = 0; j < DEEP; ++j)
 #pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (c0 + (long)j * TPB * N + k < classes) most = fmaxf(most, get(v[j], k));
-    // of terms that are all 0 so far nothing is left to rescale
-    if (most > m) s = m == -INFINITY ? s : s * scale.term(m, most);
+      for (int k = 0; k < N; ++k) most = fmaxf(most, in(j, k) ? get(v[j], k) : -INFINITY);
+    const float origin = most == -INFINITY ? 0.f : most;
+    if (most > m) s *= m == -INFINITY ? 1.f : scale.term(m, most);
     m = most;
+    float t[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < DEEP; ++j)
 #pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (c0 + (long)j * TPB * N + k < classes) s += get(v[j], k) == -INFINITY ? 0.f : scale.term(get(v[j], k), m);
+      for (int k = 0; k < N; ++k) {
+        const float e = scale.term(get(v[j], k), origin);
+        t[k & 1] += in(j, k) ? e : 0.f;
+      }
+    s += t[0] + t[1];
+  };
+  constexpr long TURN = (long)DEEP * TPB * N;
+  long c0 = threadIdx.x * N;
+  for (; c0 - threadIdx.x * N + TURN <= classes; c0 += TURN) {
+    Vec<T> v[DEEP];
+#pragma unroll
+    for (int j = 0; j < DEEP; ++j) v[j] = load_vec(x + c0 + (long)j * TPB * N, N);
+    add(v, [](int, int) { return true; });
+  }
+  if (c0 - threadIdx.x * N < classes) {
+    Vec<T> v[DEEP];
+#pragma unroll
+    for (int j = 0; j < DEEP; ++j) {
+      const long c = c0 + (long)j * TPB * N;
+      v[j] = load_vec(x + (c < classes ? c : 0), classes - c);
+    }
+    add(v, [&](int j, int k) { return c0 + (long)j * TPB * N + k < classes; });
   }
   const float mt = m;
   m = group_max<64>(m);
@@ -213,21 +228,29 @@ __global__ __launch_bounds__(1024) void policy_stream_kernel(PolicyArgs a) {
   for (long c = threadIdx.x * N; c < classes; c += TPB * N) store_gradient(scale, g, m, load_vec(x + c, classes - c), c, own, dx + c, classes - c);
 }
 
-// Which workgroup takes a row with its gradient, by the row's 16-byte groups: as few threads as hold it in registers, so that several rows
-// are on a compute unit.
+// Which workgroup takes a row, by its 16-byte groups: with its gradient as few threads as hold it in registers, so that several rows are on a
+// compute unit; without, as few as read it in some turns of four groups (16,384 x 1,000 bf16: 296 us on 1,024 threads, 55 on 256, 19 on
+// 64; 8,192 x 32,000: 157, 93; 2,048 x 151,111 fp16: 159, 145 and 139 on 512).
 template <class T>
 hipError_t run(const PolicyArgs& a, dim3 grid, hipStream_t stream) {
   const size_t groups = (a.classes + Vec<T>::N - 1) / Vec<T>::N;
 #define POLICY(TPB, NV) launch(policy_kernel<T, TPB, NV>, grid, dim3(TPB), 0, stream, a)
-  if (!a.dlogits) return launch(policy_stream_kernel<T, false>, grid, dim3(1024), 0, stream, a);
-  if (groups <= 256) return POLICY(256, 1);
+#define STREAM(TPB, GRADIENT) launch(policy_stream_kernel<T, TPB, GRADIENT>, grid, dim3(TPB), 0, stream, a)
+  if (!a.dlogits) {
+    if (groups <= 512) return STREAM(64, false);
+    if (groups <= 8192) return STREAM(256, false);
+    return STREAM(512, false);
+  }
+  if (groups <= 64) return POLICY(64, 1);
+  if (groups <= 128) return POLICY(64, 2);
+  if (groups <= 256) return POLICY(64, 4);
   if (groups <= 512) return POLICY(256, 2);
   if (groups <= 1024) return POLICY(256, 4);
   if (groups <= 2048) return POLICY(256, 8);
   if (groups <= 4096) return POLICY(512, 8);
   if (groups <= 8192) return POLICY(1024, 8);
   if (groups <= 16384) return POLICY(1024, 16);
-  return launch(policy_stream_kernel<T, true>, grid, dim3(1024), 0, stream, a);
+  return STREAM(1024, true);
 }
 
 }  // namespace
