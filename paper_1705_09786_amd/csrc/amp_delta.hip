@@ -175,14 +175,26 @@ __device__ __forceinline__ const T* past(const T* base, unsigned bytes) { return
 template <class T>
 __device__ __forceinline__ T* past(T* base, unsigned bytes) { return (T*)((char*)base + bytes); }
 
-// Four elements, n and later replaced by zeros. `fours`, the same for all lanes: n is a multiple of 4, as where dk and dv are. (A branch for
-// every count of elements instead costs the kernels' loops registers, which they spill.) p can be read where n is 0 as well.
+// Four elements, n and later replaced by zeros; p can be read where n is 0 as well. By `fours`, the same for all lanes: FOURS, n is a multiple of 4, as
+// where dk and dv are; ROWS, of a row's last elements at least four are there: they are read and moved down; NARROW, one by one. (A
+// branch for every count of elements costs the kernels' loops registers, which they spill.)
+enum { NARROW = 0, ROWS = 1, FOURS = 2 };
 template <class T>
-__device__ __forceinline__ Vec<T, 4> load_four(const T* p, int n, bool fours) {
+__device__ __forceinline__ Vec<T, 4> load_four(const T* p, int n, int fours) {
   Vec<T, 4> v;
   v.u = (typename Vec<T, 4>::U)0u;
-  if (fours) {
+  if (fours == FOURS) {
     if (n > 0) v.u = *(const typename Vec<T, 4>::Any*)p;
+  } else if (fours == ROWS) {
+    const int gone = n <= 0 || n >= 4 ? 0 : 4 - n;
+    if (n > 0) v.u = *(const typename Vec<T, 4>::Any*)(p - gone);
+    if constexpr (sizeof(T) == 2) {
+      const unsigned long x = ((unsigned long)v.u[1] << 32 | v.u[0]) >> (16 * gone);
+      v.u[0] = (unsigned)x, v.u[1] = (unsigned)(x >> 32);
+    } else {
+      if (gone & 1) v.u = (v4u){v.u[1], v.u[2], v.u[3], 0u};
+      if (gone & 2) v.u = (v4u){v.u[2], v.u[3], 0u, 0u};
+    }
   } else {
     unsigned e[4];
 #pragma unroll
@@ -199,8 +211,8 @@ __device__ __forceinline__ Vec<T, 4> load_four(const T* p, int n, bool fours) {
   return v;
 }
 template <class T>
-__device__ __forceinline__ void store_four(T* p, Vec<T, 4> v, int n, bool fours) {
-  if (fours) {
+__device__ __forceinline__ void store_four(T* p, Vec<T, 4> v, int n, int fours) {
+  if (fours == FOURS) {
     if (n > 0) *(typename Vec<T, 4>::Any*)p = v.u;
   } else {
 #pragma unroll
@@ -233,16 +245,18 @@ __device__ __forceinline__ void span(const DeltaArgs& a, size_t s, long& b, long
 // Blocks in front of a sequence, at most the workspace's number of them.
 __device__ __forceinline__ long first_block(const DeltaArgs& a, size_t s) { return a.begin ? a.first[s] : s ? (long)a.blocks : 0; }
 
-__device__ __forceinline__ bool search_block(const DeltaArgs& a, size_t index, Block& w) {
+// `first`: the plan's or, without sequences' bounds, nothing.
+__device__ __forceinline__ bool search_block(const DeltaArgs& a, const int* first, size_t index, Block& w) {
+  const auto at = [&](size_t s) { return first ? (long)first[s] : first_block(a, s); };
   size_t lo = 0, hi = a.n_seq;   // first[lo] <= index < first[hi]
-  if ((long)index >= first_block(a, hi)) return false;
+  if ((long)index >= at(hi)) return false;
   while (hi - lo > 1) {
     const size_t mid = (lo + hi) / 2;
-    (first_block(a, mid) <= (long)index ? lo : hi) = mid;
+    (at(mid) <= (long)index ? lo : hi) = mid;
   }
   long b, e;
   span(a, lo, b, e);
-  w.row = b + ((long)index - first_block(a, lo)) * B;
+  w.row = b + ((long)index - at(lo)) * B;
   w.count = e - w.row < B ? (int)(e - w.row) : B;
   w.index = index;
   return w.count > 0;
@@ -250,7 +264,7 @@ __device__ __forceinline__ bool search_block(const DeltaArgs& a, size_t index, B
 
 // The same from the plan's table: a block's first row and its rows, 0 where there is none.
 __device__ __forceinline__ bool find_block(const DeltaArgs& a, size_t index, Block& w) {
-  if (!a.begin) return search_block(a, index, w);
+  if (!a.begin) return search_block(a, nullptr, index, w);
   w.row = a.table[2 * index], w.count = a.table[2 * index + 1], w.index = index;
   return w.count > 0;
 }
@@ -308,9 +322,10 @@ __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& 
   w.first = index == 0, w.last = (long)index + 1 == count;
   return true;
 }
+__device__ __forceinline__ bool whole_sequences(const DeltaArgs& a) { return a.begin && a.first_segment[a.n_seq] == (int)a.n_seq; }
 __device__ __forceinline__ size_t first_segment(const DeltaArgs& a, size_t s) { return a.begin ? a.first_segment[s] : 0; }
 
-constexpr int PLAN = 1024;
+constexpr int PLAN = 1024, NEAR = 4096;
 // Sums in front of every thread's value; `base` goes on by the sum of all.
 __device__ __forceinline__ long sum_in_front(long mine, long& base, long (&part)[PLAN / 64]) {
   long sum = mine;
@@ -331,29 +346,41 @@ __device__ __forceinline__ long sum_in_front(long mine, long& base, long (&part)
 
 __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work) {
   __shared__ long part[PLAN / 64];
+  __shared__ int copy[NEAR + 1];   // of `first`, where it fits
+  const int* near = a.n_seq <= NEAR ? copy : a.first;
   const long most = (long)a.blocks;
-  long base = 0, longest = 0;
+  long base = 0, longest = 0, inside = 0;
   for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
     const size_t s = s0 + threadIdx.x;
     long b = 0, e = 0;
     if (s < a.n_seq) span(a, s, b, e);
     const long mine = (e - b + B - 1) / B, at = sum_in_front(mine, base, part);
     longest = mine > longest ? mine : longest;
-    if (s < a.n_seq) a.first[s] = (int)(at < most ? at : most);
+    inside += e - b;
+    if (s < a.n_seq) {
+      a.first[s] = (int)(at < most ? at : most);
+      if (a.n_seq <= NEAR) copy[s] = a.first[s];
+    }
   }
   const long all = base < most ? base : most;
-  if (threadIdx.x == 0) a.first[a.n_seq] = (int)all;
+  long sum = 0;
+  sum_in_front(inside, sum, part);
+  if (threadIdx.x == 0) {
+    a.first[a.n_seq] = (int)all;
+    if (a.n_seq <= NEAR) copy[a.n_seq] = (int)all;
+    a.first[a.n_seq + 1] = sum == (long)a.rows;   // no rows of no sequence
+  }
   __syncthreads();
   for (size_t i = threadIdx.x; i < a.blocks; i += PLAN) {
     Block w;
-    const bool in = search_block(a, i, w);
+    const bool in = search_block(a, near, i, w);
     a.table[2 * i] = in ? (int)w.row : 0, a.table[2 * i + 1] = in ? w.count : 0;
   }
   if (a.n_seq <= DELTA_ORDER && threadIdx.x < a.n_seq) {   // the longest sequences first: 24 of up to 1,350 rows on 16 heads 230 us for 300
-    const int mine = a.first[threadIdx.x + 1] - a.first[threadIdx.x];
+    const int mine = near[threadIdx.x + 1] - near[threadIdx.x];
     int front = 0;
     for (int s = 0; s < (int)a.n_seq; ++s) {
-      const int other = a.first[s + 1] - a.first[s];
+      const int other = near[s + 1] - near[s];
       front += other > mine || (other == mine && s < (int)threadIdx.x);
     }
     a.order[front] = (int)threadIdx.x;
@@ -369,7 +396,7 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
   for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
     const size_t s = s0 + threadIdx.x;
     long blocks = 0;
-    if (s < a.n_seq) blocks = a.first[s + 1] - a.first[s];   // written by this workgroup, a barrier ago
+    if (s < a.n_seq) blocks = near[s + 1] - near[s];   // written by this workgroup, a barrier ago
     const long count = s < a.n_seq ? (blocks > size ? (blocks + size - 1) / size : 1) : 0, at = sum_in_front(count, base, part);
     if (s < a.n_seq) a.first_segment[s] = (int)at;
   }
@@ -378,6 +405,7 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
 
 // Rows of no sequence: a wave to a row, zeros in every output.
 __global__ __launch_bounds__(256) void delta_zero_kernel(DeltaArgs a) {
+  if (a.n_seq && a.first[a.n_seq + 1]) return;
   for (size_t row = (size_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (size_t)gridDim.x * 4) {
     size_t lo = 0, hi = a.n_seq;   // the last sequence that begins at or in front of the row, if any
     while (lo < hi) {
@@ -707,6 +735,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
   const size_t segment = blockIdx.x / a.heads;
   const int lane = threadIdx.x % 64, c16 = lane % 16, q = lane / 16;
   Job w;
+  if (!OUT && whole_sequences(a)) return;
   if (!find_job(a, segment, w) || (!OUT && w.last)) return;
   const Columns m(a, W, !OUT && !w.first);
   const int col = m.col;
@@ -852,6 +881,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
   const size_t segment = blockIdx.x / a.heads;
   const int lane = threadIdx.x % 64, c16 = lane % 16, q = lane / 16;
   Job w;
+  if (!OUT && whole_sequences(a)) return;
   if (!find_job(a, segment, w) || (!OUT && w.first)) return;
   const Columns m(a, W, !OUT && !w.last);
   const int col = m.col;
@@ -981,6 +1011,7 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
   constexpr int PER = 32 * KT * KT * 8 / 256;
   __shared__ Matrix<3, 32 * KT, 32 * KT> map;
   const int h = blockIdx.x % a.heads;
+  if (whole_sequences(a)) return;
   const size_t s = blockIdx.x / a.heads;
   const long size = a.begin ? a.first_segment[a.n_seq + 1] : a.segment, blocks = first_block(a, s + 1) - first_block(a, s);
   const long count = blocks > size ? (blocks + size - 1) / size : 1;
@@ -1037,7 +1068,7 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
 // thread its own). Values, their gradients and the states pass in steps of 32 columns, the next on its way meanwhile, its operands in the other
 // half of the LDS. What becomes dq and dk alone, which are rounded to the inputs' type, is formed from two parts where that is a type
 // of 16 bits (2^-16 of the terms are left out); what becomes ddecay too, in 32 bits, from all.
-template <class T, int KT, bool FOURS>
+template <class T, int KT, int WIDTH>
 __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   constexpr int P = In<T>::P, PK = sizeof(T) == 2 ? 2 : 3, LV = 32 + 8, Y = P, W = P + PK, PLANES = P + PK + 3;
   constexpr bool KEEP = P < 3;   // there is room for K beside Q
@@ -1071,7 +1102,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
 #pragma unroll
     for (int j = 0; j < B * KT * 8 / 512; ++j) {
       const int i = threadIdx.x + j * 512, row = i / (KT * 8), four = i % (KT * 8), n = row < w.count ? a.dk - four * 4 : 0;
-      x[j] = load_four(past(p, n > 0 ? (row * stride + four * 4) * (unsigned)sizeof(T) : 0u), n, FOURS);
+      x[j] = load_four(past(p, n > 0 ? (row * stride + four * 4) * (unsigned)sizeof(T) : 0u), n, WIDTH);
     }
 #pragma unroll
     for (int j = 0; j < B * KT * 8 / 512; ++j) {
@@ -1112,16 +1143,16 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   const auto fetch = [&](int h, int v0) {
     const int n = in ? a.dv - v0 - col : 0, left = owner && kc < a.dk ? a.dv - v0 - 8 * q : 0;
     const size_t at = (size_t)h * a.dv + v0;
-    d = load_four(past((const T*)a.dout + w.row * a.dout_stride + at, n > 0 ? d_at : 0u), n, FOURS);
-    v = load_four(past((const T*)a.v + w.row * a.v_stride + at, n > 0 ? v_at : 0u), n, FOURS);
-    ev = load_four(past(a.carry_in + w.row * wide + at, n > 0 ? e_at : 0u), n, FOURS);
-    xv = load_four(past(a.x + w.row * wide + at, n > 0 ? e_at : 0u), n, FOURS);
+    d = load_four(past((const T*)a.dout + w.row * a.dout_stride + at, n > 0 ? d_at : 0u), n, WIDTH);
+    v = load_four(past((const T*)a.v + w.row * a.v_stride + at, n > 0 ? v_at : 0u), n, WIDTH);
+    ev = load_four(past(a.carry_in + w.row * wide + at, n > 0 ? e_at : 0u), n, WIDTH);
+    xv = load_four(past(a.x + w.row * wide + at, n > 0 ? e_at : 0u), n, WIDTH);
     const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h) + v0;
     const float* behind = a.behind + state_at(a, w.index, h) + v0;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      s0[k] = load_four(past(before + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, FOURS);
-      s1[k] = load_four(past(behind + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, FOURS);
+      s0[k] = load_four(past(before + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, WIDTH);
+      s1[k] = load_four(past(behind + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, WIDTH);
     }
 };
   fetch(hk * group, 0);
@@ -1160,7 +1191,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
           e[i] = b * get(ev, i);
           dvv = fmaf(y[i], get(v, i), dvv);
         }
-        store_four((T*)a.dvalue + (w.row + row) * a.dv_stride + at + col, pack<T>(y), n, FOURS);
+        store_four((T*)a.dvalue + (w.row + row) * a.dv_stride + at + col, pack<T>(y), n, WIDTH);
         v2u x[3], yp[PK], z[P];
         parts4(d, z);
 #pragma unroll
@@ -1465,7 +1496,7 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk,
     at += (bytes + 255) / 256 * 256;
     return p;
   };
-  s.first = take((n + 1) * sizeof(int));
+  s.first = take((n + 2) * sizeof(int));
   s.first_segment = take((n + 2) * sizeof(int));
   s.order = take(n <= DELTA_ORDER ? n * sizeof(int) : 0);
   s.table = take(s.blocks * 2 * sizeof(int));
@@ -1487,7 +1518,7 @@ unsigned groups_of(size_t tiles) { return tiles <= 4 ? 1 : (unsigned)((tiles + 7
 void lay_out(DeltaArgs& a, bool backward) {
   const Sizes s = sizes_of(a.rows, a.n_seq, a.heads, a.key_heads, a.dk, a.dv, backward);
   char* w = (char*)a.workspace;
-  a.fours = a.dk % 4 == 0 && a.dv % 4 == 0;
+  a.fours = a.dk % 4 == 0 && a.dv % 4 == 0 ? FOURS : a.dk >= 4 && a.dv >= 4 ? ROWS : NARROW;
   a.blocks = s.blocks;
   a.segments = s.segments;
   a.first = (int*)(w + s.first);
@@ -1517,7 +1548,7 @@ hipError_t plan(DeltaArgs& a, hipStream_t stream) {
   }
   const size_t groups = (a.rows + 3) / 4;
   if (e == hipSuccess && a.zero_others && a.rows && (a.begin || !a.n_seq))
-    e = launch(delta_zero_kernel, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, stream, a);
+    e = launch(delta_zero_kernel, dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, stream, a);
   return e;
 }
 
@@ -1559,8 +1590,9 @@ hipError_t backward(const DeltaArgs& a, hipStream_t stream) {
   e = a.dv <= 64 ? chain<T, KT, 4, true>(a, stream) : chain<T, KT, 8, true>(a, stream);
   if (e != hipSuccess || !a.blocks) return e;
   const dim3 grid((unsigned)(a.blocks * a.key_heads));
-  if (a.fours) return launch(delta_gradient_kernel<T, KT, true>, grid, dim3(512), 0, stream, a);
-  return launch(delta_gradient_kernel<T, KT, false>, grid, dim3(512), 0, stream, a);
+  if (a.fours == FOURS) return launch(delta_gradient_kernel<T, KT, FOURS>, grid, dim3(512), 0, stream, a);
+  if (a.fours == ROWS) return launch(delta_gradient_kernel<T, KT, ROWS>, grid, dim3(512), 0, stream, a);
+  return launch(delta_gradient_kernel<T, KT, NARROW>, grid, dim3(512), 0, stream, a);
 }
 
 #define BY_KEY(CALL)                  \
