@@ -276,6 +276,12 @@ __device__ __forceinline__ float* matrices_of(const DeltaArgs& a, size_t block, 
 }
 __device__ __forceinline__ float* scalars_of(const DeltaArgs& a, size_t block, int h) { return a.scalars + (block * a.heads + h) * (4 * B); }
 __device__ __forceinline__ double* sums_of(const DeltaArgs& a, size_t block, int h) { return a.sums + (block * a.heads + h) * B; }
+// What the gradients are formed from lies block by block and head by head in tiles of 16 columns, as the chain's waves have them, so that both
+// sides read and write memory in one piece: E and X 64 rows to a tile, states dk; columns behind the last are zeros.
+__device__ __forceinline__ int tiled_columns(const DeltaArgs& a) { return (a.dv + 15) / 16 * 16; }
+__device__ __forceinline__ size_t rows_at(const DeltaArgs& a, size_t block, int h) { return (block * a.heads + h) * ((size_t)B * tiled_columns(a)); }
+__device__ __forceinline__ size_t tiles_at(const DeltaArgs& a, size_t block, int h) { return (block * a.heads + h) * ((size_t)a.dk * tiled_columns(a)); }
+
 __device__ __forceinline__ size_t state_at(const DeltaArgs& a, size_t index, int h) { return (index * a.heads + h) * ((size_t)a.dk * a.dv); }
 
 // ------------------------------------------------------------------ plan
@@ -694,6 +700,15 @@ struct State {
       for (int i = 0; i < 4; ++i)
         if (dk == 32 * KT || 16 * m + r0 + i < dk) *past(p + (16 * m + i) * width, (unsigned)(r0 * width + col) * 4u) = t[m][i];
   }
+  // to a tile of 16 columns
+  __device__ __forceinline__ void store_tile(float* p, int dk) const {
+    const int r0 = 4 * (threadIdx.x % 64 / 16);
+#pragma unroll
+    for (int m = 0; m < 2 * KT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (dk == 32 * KT || 16 * m + r0 + i < dk) *past(p + (16 * m + i) * 16, (unsigned)(r0 * 16 + threadIdx.x % 16) * 4u) = t[m][i];
+  }
   __device__ __forceinline__ void identity(int col) {
     const int r0 = 4 * (threadIdx.x % 64 / 16);
 #pragma unroll
@@ -749,7 +764,8 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
   else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
   else S.identity(m.map ? col : -1);
   const T* V = (const T*)a.v + (size_t)h * a.dv;
-  const unsigned vcol = m.map || col >= a.dv ? 0 : col, vlane = (4u * q * (unsigned)a.v_stride + vcol) * (unsigned)sizeof(T);
+  const bool none = m.map || col >= a.dv;   // no values: a map's columns, and those behind the last
+  const unsigned vcol = none ? 0 : col, vlane = (4u * q * (unsigned)a.v_stride + vcol) * (unsigned)sizeof(T);
   const int chunks = (int)((e - b + C - 1) / C);
   const auto rows_in = [&](int c) { return e - b - (long)c * C < C ? (int)(e - b - (long)c * C) : C; };
   Ck next(a);
@@ -773,7 +789,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
     v4f oq[2] = {};
     float x[8], y[8];
     if (m.any) {
-      if (OUT && a.carry && c % 2 == 0) S.store(a.carry + a.carry_states + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
+      if (OUT && a.carry && c % 2 == 0) S.store_tile(a.carry + a.carry_states + tiles_at(a, (size_t)(first + c / 2), h) + m.c0 * a.dk, a.dk);
       v4f ks[2] = {};
       Frag<In<T>::P> kf[2][2], qf[2][2];
       const auto read = [&](int f) {
@@ -805,7 +821,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
       on_their_way<OUT>();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        x[k] = (m.map ? 0.f : widen((OUT ? v : vnext).v[k])) - grow[k] * ks[k / 4][k % 4];
+        x[k] = (none ? 0.f : widen((OUT ? v : vnext).v[k])) - grow[k] * ks[k / 4][k % 4];
         y[k] = beta[k] * x[k];
       }
       const Frag<3> rb = split8<3>(y);
@@ -817,13 +833,10 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
     if (!OUT && c + 1 < chunks) fetch(c + 1);
     if (m.any) {
       const Eight beta(t.beta), rest(t.rest);
-      if (OUT && a.carry && col < a.dv) {
-        const size_t wide = (size_t)a.heads * a.dv;
-        float* E = a.carry + row * wide + (size_t)h * a.dv;
-        const unsigned at = (4u * q * (unsigned)wide + col) * 4u;
+      if (OUT && a.carry) {
+        float* E = a.carry + rows_at(a, (size_t)(first + c / 2), h) + (m.c0 * B + c % 2 * C * 16);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (count == C || chunk_row(k) < count) *past(E + ((k / 4) * 16 + k % 4) * wide, at) = x[k];
+        for (int k = 0; k < 8; ++k) *past(E + ((k / 4) * 16 + k % 4) * 16, (unsigned)(4 * q * 16 + c16) * 4u) = x[k];
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -895,7 +908,8 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
   else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
   else S.identity(m.map ? col : -1);
   const T* D = (const T*)a.dout + (size_t)h * a.dv;
-  const unsigned dcol = m.map || col >= a.dv ? 0 : col, dlane = (4u * q * (unsigned)a.dout_stride + dcol) * (unsigned)sizeof(T);
+  const bool none = m.map || col >= a.dv;
+  const unsigned dcol = none ? 0 : col, dlane = (4u * q * (unsigned)a.dout_stride + dcol) * (unsigned)sizeof(T);
   const int chunks = (int)((e - b + C - 1) / C);
   const auto rows_in = [&](int c) { return e - b - (long)c * C < C ? (int)(e - b - (long)c * C) : C; };
   Ck next(a);
@@ -919,7 +933,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     float x[8], y[8];
     Frag<3> od;
     if (m.any) {
-      if (OUT && (c % 2 || c == chunks - 1)) S.store(a.behind + state_at(a, (size_t)(first + c / 2), h), a.dk, a.dv, col);
+      if (OUT && (c % 2 || c == chunks - 1)) S.store_tile(a.behind + tiles_at(a, (size_t)(first + c / 2), h) + m.c0 * a.dk, a.dk);
       v4f ks[2] = {};
       Frag<P> kf[2][2];
       const auto read = [&](int f) {
@@ -946,7 +960,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       for (int r = 0; r < 2; ++r) nf[r] = t.n.down(r, 0);
       on_their_way<OUT>();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = m.map ? 0.f : widen((OUT ? d : dnext).v[k]);
+      for (int k = 0; k < 8; ++k) x[k] = none ? 0.f : widen((OUT ? d : dnext).v[k]);
       const Frag<P> dop = split8<P>(x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -972,13 +986,10 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       Frag<P> kd[2], qd[2];
       kd[0] = t.k.down(0, 0), qd[0] = t.q.down(0, 0);
       on_their_way<OUT>();
-      if (OUT && col < a.dv) {
-        const size_t wide = (size_t)a.heads * a.dv;
-        float* X = a.x + row * wide + (size_t)h * a.dv;
-        const unsigned at = (4u * q * (unsigned)wide + col) * 4u;
+      if (OUT) {
+        float* X = a.x + rows_at(a, (size_t)(first + c / 2), h) + (m.c0 * B + c % 2 * C * 16);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (count == C || chunk_row(k) < count) *past(X + ((k / 4) * 16 + k % 4) * wide, at) = x[k];
+        for (int k = 0; k < 8; ++k) *past(X + ((k / 4) * 16 + k % 4) * 16, (unsigned)(4 * q * 16 + c16) * 4u) = x[k];
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] = -grow[k] * beta[k] * x[k];
@@ -1133,28 +1144,30 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
 #pragma unroll
       for (int f = 0; f < KT; ++f) qk[k] = mma<3>(kq.along(16 * it, f), km.along(16 * jt, f), qk[k]);
     }
-  const size_t wide = (size_t)a.heads * a.dv;
   const int row = threadIdx.x / 8, col = 4 * (threadIdx.x % 8);
   const bool in = row < w.count;
   const unsigned d_at = (row * (unsigned)a.dout_stride + col) * (unsigned)sizeof(T), v_at = (row * (unsigned)a.v_stride + col) * (unsigned)sizeof(T);
-  const unsigned e_at = (row * (unsigned)wide + col) * 4u, s_at = ((unsigned)kc * a.dv + 8 * q) * 4u;
+  const unsigned e_at = (unsigned)(col / 16 * (B * 16) + row * 16 + col % 16) * 4u, s_at = (unsigned)(q / 2 * (a.dk * 16) + kc * 16 + q % 2 * 8) * 4u;
+  const int tiled = tiled_columns(a);
   Vec<T, 4> d, v;
   Vec<float, 4> ev, xv, s0[2], s1[2];
   const auto fetch = [&](int h, int v0) {
-    const int n = in ? a.dv - v0 - col : 0, left = owner && kc < a.dk ? a.dv - v0 - 8 * q : 0;
+    const int n = in ? a.dv - v0 - col : 0;
     const size_t at = (size_t)h * a.dv + v0;
     d = load_four(past((const T*)a.dout + w.row * a.dout_stride + at, n > 0 ? d_at : 0u), n, WIDTH);
     v = load_four(past((const T*)a.v + w.row * a.v_stride + at, n > 0 ? v_at : 0u), n, WIDTH);
-    ev = load_four(past(a.carry_in + w.row * wide + at, n > 0 ? e_at : 0u), n, WIDTH);
-    xv = load_four(past(a.x + w.row * wide + at, n > 0 ? e_at : 0u), n, WIDTH);
-    const float* before = a.carry_in + a.carry_states + state_at(a, w.index, h) + v0;
-    const float* behind = a.behind + state_at(a, w.index, h) + v0;
+    // a tile's columns are all there, zeros behind the last
+    const int rows = in && v0 + col < tiled ? 4 : 0, states = owner && kc < a.dk && v0 + 8 * q < tiled ? 4 : 0;
+    ev = load_four(past(a.carry_in + rows_at(a, w.index, h) + v0 * B, rows ? e_at : 0u), rows, FOURS);
+    xv = load_four(past(a.x + rows_at(a, w.index, h) + v0 * B, rows ? e_at : 0u), rows, FOURS);
+    const float* before = a.carry_in + a.carry_states + tiles_at(a, w.index, h) + v0 * a.dk;
+    const float* behind = a.behind + tiles_at(a, w.index, h) + v0 * a.dk;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      s0[k] = load_four(past(before + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, WIDTH);
-      s1[k] = load_four(past(behind + 4 * k, left - 4 * k > 0 ? s_at : 0u), left - 4 * k, WIDTH);
+      s0[k] = load_four(past(before + 4 * k, states ? s_at : 0u), states, FOURS);
+      s1[k] = load_four(past(behind + 4 * k, states ? s_at : 0u), states, FOURS);
     }
-};
+  };
   fetch(hk * group, 0);
   int turn = 0;
   // the group's sums: dq's and dk's 16 values of this thread, and dP's and dM's 12
@@ -1503,8 +1516,9 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk,
   s.matrices = take(s.blocks * heads * 4 * C * C * sizeof(float));
   s.scalars = take(s.blocks * heads * 4 * B * sizeof(float));
   s.sums = take(s.blocks * heads * B * sizeof(double));
-  s.x = take(backward ? rows * heads * dv * sizeof(float) : 0);
-  s.behind = take(backward ? s.blocks * heads * dk * dv * sizeof(float) : 0);
+  const size_t tiled = (dv + 15) / 16 * 16;
+  s.x = take(backward ? s.blocks * heads * B * tiled * sizeof(float) : 0);
+  s.behind = take(backward ? s.blocks * heads * dk * tiled * sizeof(float) : 0);
   s.kept = take(backward && heads > key_heads ? s.blocks * key_heads * 44 * 512 * sizeof(float) : 0);
   s.fronts = take(s.segments * heads * dk * dv * sizeof(float));
   s.maps = take(s.segments * heads * dk * dk * sizeof(float));
@@ -1533,7 +1547,7 @@ void lay_out(DeltaArgs& a, bool backward) {
   a.kept = (float*)(w + s.kept);
   a.fronts = (float*)(w + s.fronts);
   a.maps = (float*)(w + s.maps);
-  a.carry_states = a.rows * a.heads * a.dv;
+  a.carry_states = s.blocks * a.heads * B * ((a.dv + 15) / 16 * 16);
 }
 
 hipError_t plan(DeltaArgs& a, hipStream_t stream) {

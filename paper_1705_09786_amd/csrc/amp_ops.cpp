@@ -179,7 +179,7 @@ void delta_in(DeltaArgs& a, const amp_delta_shape* s, const DeltaIn& q, const De
 }
 
 size_t delta_carry_floats(const amp_delta_shape* s, size_t n) {
-  return s->rows * s->heads * s->dv + amp_delta_blocks(s->rows, n) * s->heads * s->dk * s->dv;
+  return amp_delta_blocks(s->rows, n) * s->heads * (DELTA_BLOCK + s->dk) * ((s->dv + 15) / 16 * 16);
 }
 
 constexpr size_t MAX_TENSORS = (size_t)1 << 20, MAX_ELEMENTS = (size_t)1 << 40;
@@ -494,7 +494,7 @@ int amp_gated_delta_backward(const amp_delta_shape* shape, const void* dout, siz
     REQUIRE(v);
     REQUIRE(decay);
     REQUIRE(beta);
-    REQUIRE(carry);
+    if (n) REQUIRE(carry);
     REQUIRE(dq);
     REQUIRE(dk);
     REQUIRE(dv);

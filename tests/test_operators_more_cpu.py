@@ -129,7 +129,7 @@ def test_delta_sizes():
     lib = B.lib()
     s = B.DeltaShape(*SHAPE.values())
     assert lib.amp_gated_delta_carry(s, 3, ct.byref(n)) == B.AMP_OK
-    assert n.value == 100 * 64 + (100 // 64 + 3) * 4 * 8 * 16
+    assert n.value == (100 // 64 + 3) * 4 * (64 + 8) * 16
     sizes = []
     for back in (0, 1):
         assert lib.amp_gated_delta_workspace(s, 3, back, ct.byref(n)) == B.AMP_OK
