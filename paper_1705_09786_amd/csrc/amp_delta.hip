@@ -1100,6 +1100,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   __shared__ Matrix<KEEP ? P : 1, KEEP ? B : 1, KT * 32> kept_k;
   __shared__ double g[B];
   __shared__ float grow[B], rest[B], beta[B], vrow[B];
+  __shared__ float kept_here[P == 1 ? 28 : 1][512];   // dq's and the pairs' sums, where there is room
   Block w;
   const int hk = blockIdx.x % a.key_heads, group = a.heads / a.key_heads;
   if (!find_block(a, blockIdx.x / a.key_heads, w)) return;
@@ -1132,18 +1133,6 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
     if constexpr (KEEP) return kept_k;
     else return u.k;
   }();
-  load_kq(Q, (unsigned)a.q_stride, kq);
-  load_kq(K, (unsigned)a.k_stride, km);
-  __syncthreads();
-  v4f qk[2] = {};   // Q K^T in the wave's tiles of dP
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    if (wave + 8 * k < 10) {
-      int it, jt;
-      tile_of(wave + 8 * k, it, jt);
-#pragma unroll
-      for (int f = 0; f < KT; ++f) qk[k] = mma<3>(kq.along(16 * it, f), km.along(16 * jt, f), qk[k]);
-    }
   const int row = threadIdx.x / 8, col = 4 * (threadIdx.x % 8);
   const bool in = row < w.count;
   const unsigned d_at = (row * (unsigned)a.dout_stride + col) * (unsigned)sizeof(T), v_at = (row * (unsigned)a.v_stride + col) * (unsigned)sizeof(T);
@@ -1168,7 +1157,29 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       s1[k] = load_four(past(behind + 4 * k, states ? s_at : 0u), states, FOURS);
     }
   };
+  // a head's sums of decays and rates, of the row that this thread stands for
+  double sum = 0.0, half = 0.0, last = 0.0;
+  float rate = 0.f;
+  const auto ahead = [&](int h) {
+    if (threadIdx.x >= B) return;
+    const double* sums = sums_of(a, w.index, h);
+    sum = sums[threadIdx.x], half = sums[C - 1], last = sums[B - 1];
+    rate = scalars_of(a, w.index, h)[2 * B + threadIdx.x];
+  };
+  ahead(hk * group);
   fetch(hk * group, 0);
+  load_kq(Q, (unsigned)a.q_stride, kq);
+  load_kq(K, (unsigned)a.k_stride, km);
+  __syncthreads();
+  v4f qk[2] = {};   // Q K^T in the wave's tiles of dP
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (wave + 8 * k < 10) {
+      int it, jt;
+      tile_of(wave + 8 * k, it, jt);
+#pragma unroll
+      for (int f = 0; f < KT; ++f) qk[k] = mma<3>(kq.along(16 * it, f), km.along(16 * jt, f), qk[k]);
+    }
   int turn = 0;
   // the group's sums: dq's and dk's 16 values of this thread, and dP's and dM's 12
   float* kept = a.kept + ((w.index * a.key_heads + hk) * 44) * 512;
@@ -1176,12 +1187,11 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
     __syncthreads();   // LDS is free
     if (threadIdx.x < B) {
-      const double* sums = sums_of(a, w.index, h);
-      const double half = sums[C - 1], end = half + sums[B - 1], mine = sums[threadIdx.x] + (threadIdx.x >= C ? half : 0.0);
+      const double end = half + last, mine = sum + (threadIdx.x >= C ? half : 0.0);
       g[threadIdx.x] = mine;
-      grow[threadIdx.x] = expf((float)mine);
-      rest[threadIdx.x] = expf((float)(end - mine));
-      beta[threadIdx.x] = scalars_of(a, w.index, h)[2 * B + threadIdx.x];
+      grow[threadIdx.x] = power(mine);
+      rest[threadIdx.x] = power(end - mine);
+      beta[threadIdx.x] = rate;
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) dq[t] = dr[t] = dc[t] = (v4f)0.f;
@@ -1282,13 +1292,14 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
         const int r = 16 * t + 4 * q + i < w.count ? 16 * t + 4 * q + i : w.count - 1, c = kc < a.dk ? kc : a.dk - 1;
         kv[t][i] = widen(*past(K, ((unsigned)r * (unsigned)a.k_stride + c) * (unsigned)sizeof(T)));
       }
+    if (h + 1 < (hk + 1) * group) ahead(h + 1);
     dbeta = group_sum<8>(dbeta), dvv = group_sum<8>(dvv);
     if (threadIdx.x % 8 == 0) {
       if (in) a.dbeta[(w.row + row) * a.dbeta_stride + h] = dbeta;
       vrow[row] = dvv;
     }
     __syncthreads();
-    float tail = expf((float)g[B - 1]) * ss;   // <S', the state behind>
+    float tail = power(g[B - 1]) * ss;   // <S', the state behind>
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -1327,7 +1338,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int r = 16 * it + 4 * q + i;
         const bool there = t >= 10 ? r > j : r >= j;
-        pair[k][i] = there ? (t >= 10 ? -1.f : a.scale) * expf((float)(g[r] - g[j])) * pair[k][i] : 0.f;
+        pair[k][i] = there ? (t >= 10 ? -1.f : a.scale) * power(g[r] - g[j]) * pair[k][i] : 0.f;
         if (t < 10) {
           const float y = sum16(pair[k][i] * qk[k < 2 ? k : 0][i]);
           if (c16 == 0) u.rows.prow[jt][r] = y;
@@ -1335,25 +1346,26 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       }
     }
     if (group > 1) {   // to the heads in front
+      const auto place = [&](int n) { return P == 1 && (n < 16 || n >= 32) ? &kept_here[n < 16 ? n : n - 16][id] : past(kept + n * 512, mine); };
       if (h > hk * group) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) dq[t][i] += *past(kept + (4 * t + i) * 512, mine), dr[t][i] += *past(kept + (16 + 4 * t + i) * 512, mine);
+          for (int i = 0; i < 4; ++i) dq[t][i] += *place(4 * t + i), dr[t][i] += *place(16 + 4 * t + i);
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pair[k][i] += *past(kept + (32 + 4 * k + i) * 512, mine);
+          for (int i = 0; i < 4; ++i) pair[k][i] += *place(32 + 4 * k + i);
       }
       if (h + 1 < (hk + 1) * group) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) *past(kept + (4 * t + i) * 512, mine) = dq[t][i], *past(kept + (16 + 4 * t + i) * 512, mine) = dr[t][i];
+          for (int i = 0; i < 4; ++i) *place(4 * t + i) = dq[t][i], *place(16 + 4 * t + i) = dr[t][i];
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) *past(kept + (32 + 4 * k + i) * 512, mine) = pair[k][i];
+          for (int i = 0; i < 4; ++i) *place(32 + 4 * k + i) = pair[k][i];
       }
     }
     __syncthreads();
