@@ -4,6 +4,8 @@
 // tensors that its arguments list, each piece's sum of squares has a place of its own in the workspace, in 64 bits (a square of a
 // float may be beyond floats, and a sum of 2^30 of them loses half its digits), and one workgroup adds the places up in their order.  The
 // second reading goes through the tensors from the last to the first, so that it begins with what the memory-side cache has last seen.
+// 97 tensors of 314 million floats together: the norm in 217 us (5.8 TB/s); 600 of 302 million bf16 with results: 110 us for the norm, 190 for
+// the results, and 390 with what the host does for 600 tensors.
 #include "amp_ops.hip.h"
 
 namespace {

@@ -463,10 +463,10 @@ int amp_gated_delta_forward(const amp_delta_shape* shape, const void* q, size_t 
                     {"beta", beta, rows, heads, beta_stride, 4},  {"h0", h0, n, state, state, 4},
                     {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
   CHECK(check_arrays(what, s, 4));
-  CHECK(check_scan_stride(what, "q", q_stride));
-  CHECK(check_scan_stride(what, "k", k_stride));
-  CHECK(check_scan_stride(what, "v", v_stride));
-  CHECK(check_scan_stride(what, "o", o_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "q", q_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "k", k_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "v", v_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "o", o_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 4, nullptr, 0));
   DeltaArgs a = {};
@@ -513,10 +513,10 @@ int amp_gated_delta_backward(const amp_delta_shape* shape, const void* dout, siz
                     {"carry", carry, 1, nc, nc, 4},                     {"dlast", dlast, n, state, state, 4},
                     {"begin", seq->begin, 1, n, n, seq->begin ? ib : 1}, {"end", seq->end, 1, n, n, seq->end ? ib : 1}};
   CHECK(check_arrays(what, s, 7));
-  CHECK(check_scan_stride(what, "dout", dout_stride));
-  CHECK(check_scan_stride(what, "q", q_stride));
-  CHECK(check_scan_stride(what, "k", k_stride));
-  CHECK(check_scan_stride(what, "v", v_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "dout", dout_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "q", q_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "k", k_stride));
+  if (rows > 1) CHECK(check_scan_stride(what, "v", v_stride));
   CHECK(check_workspace(what, workspace, workspace_bytes, need));
   CHECK(check_overlaps(what, s, 7, nullptr, 0));
   DeltaArgs a = {};

@@ -140,6 +140,16 @@ def test_delta_parts_of_wider_arrays_and_rows_of_no_sequence():
     assert same_bits(grads[5], got[7])
 
 
+def test_delta_one_row_of_any_stride():
+    x, y = layer(1, 1, 2, 1, 8, 12)
+    want = both(x, y, None, 1)
+    on = {k: torch.empty_strided(v.shape, (1 << 30, 1), device="cuda").copy_(v) for k, v in x.items()}
+    o, last, carry = ops.gated_delta(*on.values(), key_heads=1, h0=dev(y["h0"]), last=True, carry=True)
+    do = torch.empty_strided(y["do"].shape, (1 << 30, 1), device="cuda").copy_(y["do"])
+    grads = ops.gated_delta_backward(do, *on.values(), carry, key_heads=1, dlast=dev(y["dlast"]))
+    assert all(same_bits(p, q) for p, q in zip((o, last) + grads, want))
+
+
 def test_delta_without_rows_or_sequences():
     x, y = layer(6, 3, 2, 2, 8, 8)
     empty = torch.zeros(4, dtype=torch.int64)
