@@ -867,14 +867,16 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
           }
         }
       }
-      Frag<In<T>::P> kd[2];
-      kd[0] = t.k.down(0, 0);
+      Frag<In<T>::P> kd[2][2];
+      kd[0][0] = t.k.down(0, 0), kd[0][1] = t.k.down(1, 0);
       const Frag<3> up = split8<3>(y);
 #pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) {
-        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0);
+      for (int i = 0; i < KT; ++i) {
+        if (i + 1 < KT) kd[(i + 1) % 2][0] = t.k.down(2 * i + 2, 0), kd[(i + 1) % 2][1] = t.k.down(2 * i + 3, 0);
         on_their_way<OUT>();
-        S.t[i] = mma<3>(kd[i % 2], up, S.t[i]);
+        v4f two[2] = {S.t[2 * i], S.t[2 * i + 1]};
+        mma2<3>(kd[i % 2], up, two);
+        S.t[2 * i] = two[0], S.t[2 * i + 1] = two[1];
       }
     }
     if (c + 1 < chunks) next.put(sh[(c + 1) & 1]);
@@ -990,8 +992,9 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
     if (!OUT && c > 0) fetch(c - 1);
     if (m.any) {
       const Eight grow(t.grow), beta(t.beta);
-      Frag<P> kd[2], qd[2];
-      kd[0] = t.k.down(0, 0), qd[0] = t.q.down(0, 0);
+      Frag<P> kd[2][2], qd[2][2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) kd[0][z] = t.k.down(z, 0), qd[0][z] = t.q.down(z, 0);
       on_their_way<OUT>();
       if (OUT) {
         float* X = a.x + rows_at(a, (size_t)(first + c / 2), h) + (m.c0 * B + c % 2 * C * 16);
@@ -1002,10 +1005,15 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
       for (int k = 0; k < 8; ++k) y[k] = -grow[k] * beta[k] * x[k];
       const Frag<3> down = split8<3>(y);
 #pragma unroll
-      for (int i = 0; i < 2 * KT; ++i) {
-        if (i + 1 < 2 * KT) kd[(i + 1) % 2] = t.k.down(i + 1, 0), qd[(i + 1) % 2] = t.q.down(i + 1, 0);
+      for (int i = 0; i < KT; ++i) {
+        if (i + 1 < KT)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) kd[(i + 1) % 2][z] = t.k.down(2 * i + 2 + z, 0), qd[(i + 1) % 2][z] = t.q.down(2 * i + 2 + z, 0);
         on_their_way<OUT>();
-        S.t[i] = mma<3>(kd[i % 2], down, mma<3>(qd[i % 2], od, S.t[i]));
+        v4f two[2] = {S.t[2 * i], S.t[2 * i + 1]};
+        mma2<3>(qd[i % 2], od, two);
+        mma2<3>(kd[i % 2], down, two);
+        S.t[2 * i] = two[0], S.t[2 * i + 1] = two[1];
       }
     }
     if (c > 0) next.put(sh[(c - 1) & 1]);
@@ -1608,12 +1616,21 @@ hipError_t chain(const DeltaArgs& a, hipStream_t stream) {
   else return launch(delta_forward_kernel<T, KT, W, true>, dim3(x, groups(values)), dim3(64 * W), 0, stream, a);
 }
 
+// Whether a sequence and head's columns go to workgroups of four waves instead of eight: where four have them all, and where types of several
+// parts, whose waves do more, leave half of the compute units without a workgroup of eight (8 sequences of 1,024 rows, 8 heads of 128 x
+// 128, either direction: f32 238 us in eights, 178 in fours, fp16 184 and 154, bf16 152 and 159; with 24 sequences and 16 heads bf16 300 and 400).
+template <class T>
+bool in_fours(const DeltaArgs& a) {
+  const size_t eights = a.n_seq * a.heads * ((a.dv + 127) / 128);
+  return a.dv <= 64 || (In<T>::P > 1 && eights <= 128 && a.rows / B < 24 * a.n_seq);
+}
+
 template <class T, int KT>
 hipError_t forward(const DeltaArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.blocks) e = prepare<T, KT>(a, stream);
   if (e != hipSuccess || !a.n_seq) return e;
-  return a.dv <= 64 ? chain<T, KT, 4, false>(a, stream) : chain<T, KT, 8, false>(a, stream);
+  return in_fours<T>(a) ? chain<T, KT, 4, false>(a, stream) : chain<T, KT, 8, false>(a, stream);
 }
 
 template <class T, int KT>
@@ -1621,7 +1638,7 @@ hipError_t backward(const DeltaArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.blocks) e = prepare<T, KT>(a, stream);
   if (e != hipSuccess || !a.n_seq) return e;
-  e = a.dv <= 64 ? chain<T, KT, 4, true>(a, stream) : chain<T, KT, 8, true>(a, stream);
+  e = in_fours<T>(a) ? chain<T, KT, 4, true>(a, stream) : chain<T, KT, 8, true>(a, stream);
   if (e != hipSuccess || !a.blocks) return e;
   const dim3 grid((unsigned)(a.blocks * a.key_heads));
   if (a.fours == FOURS) return launch(delta_gradient_kernel<T, KT, FOURS>, grid, dim3(512), 0, stream, a);
