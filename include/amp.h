@@ -467,8 +467,10 @@ int amp_measure_peaks(void *dev_buf, size_t bytes, void *hip_stream, double *lds
  * products when it runs over whole token arrays instead of message by
  * message: the layer norm, the GRU's state update with gates that do not
  * read the state (Section 2 lists the GRU among the cells; Appendix C has
- * its update), and a loss layer against a teacher's top logits.  They need
- * no context.
+ * its update), and a loss layer against a teacher's top logits; and for one
+ * with matrix states that is trained by rewards the gated delta rule, a
+ * clipped policy loss, and the gradients' norm with clipping.  They need no
+ * context.
  *
  * Conventions
  *   - Every array is DEVICE memory, on the device that is current at the

@@ -1,5 +1,5 @@
-// C entry points of the operators on whole arrays (include/amp.h): argument checks and launches.  Nothing here allocates, waits or
-// throws.
+// C entry points of the operators on whole arrays (include/amp.h): argument checks and launches.  Nothing here allocates (but a list of host
+// memory, while clipping's results are checked), waits or throws.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>

@@ -1,5 +1,5 @@
 // What the checks (amp_ops.cpp) and the kernels of the operators on whole arrays (amp_norm.hip, amp_scan.hip,
-// amp_distill.hip) agree on: arguments and launchers.  Sizes have been checked when a launcher is called.
+// amp_distill.hip, amp_delta.hip, amp_policy.hip, amp_clip.hip) agree on: arguments and launchers.  Sizes have been checked when a launcher is called.
 #pragma once
 #include <hip/hip_runtime_api.h>
 #include <stddef.h>

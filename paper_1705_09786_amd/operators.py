@@ -1,5 +1,5 @@
-"""The operators on whole arrays over torch tensors: layer norm, the gated linear recurrence, the distillation loss (include/amp.h has
-their formulas and conventions).  Marshalling only, as in runner: outputs and workspaces come from torch, the kernels run on
+"""The operators on whole arrays over torch tensors: layer norm, the gated linear recurrence and the gated delta rule, the distillation and the
+policy loss, the gradients' norm and clipping (include/amp.h has their formulas and conventions).  Marshalling only, as in runner: outputs and workspaces come from torch, the kernels run on
 torch's current stream of the tensors' device, and a refused call raises binding.AmpError.
 
 Arrays are 2-D tensors (rows, features) on one GPU, torch.float32, bfloat16 or float16, features next to each other, any row stride;

@@ -28,6 +28,8 @@ def _flat(x):
 
 
 def _sum(n):
+    """Units of a sum of n products. (A power e^x of a chunk's decays is off by |x| units, its exponent being rounded to 24 bits, and is 0 below x =
+    -104: less than this from n = 14 on, the fewest keys that are tested with decays as strong.)"""
     return 6 * n + 24
 
 

@@ -173,6 +173,26 @@ def test_delta_bounds_outside_the_rows():
     torch.cuda.synchronize()
 
 
+def test_delta_thousands_of_sequences():
+    """More than the plan keeps near: the same bits as in two calls for half of them each."""
+    n = 6001
+    lengths = torch.randint(0, 4, (n,), generator=torch.Generator().manual_seed(1))
+    lengths[3000] = 200
+    where = offsets(*lengths.tolist())
+    rows, half = int(where[-1]), 3000
+    x, y = layer(rows, n, 1, 1, 8, 8)
+    got = both(x, y, where, 1)
+    cut = int(where[half])
+    parts = [both({k: v[:cut] for k, v in x.items()}, dict(h0=y["h0"][:half], do=y["do"][:cut], dlast=y["dlast"][:half]), where[:half + 1], 1),
+             both({k: v[cut:] for k, v in x.items()}, dict(h0=y["h0"][half:], do=y["do"][cut:], dlast=y["dlast"][half:]), where[half:] - cut, 1)]
+    for i, g in enumerate(got):
+        assert same_bits(g, torch.cat([p[i] for p in parts]))
+    some = slice(int(where[2990]), int(where[3010]))
+    want = more.delta(*(t[some] for t in x.values()), where[2990:3011] - where[2990], 1, None, y["h0"][2990:3010], torch.float32)
+    check("o", got[0][some], want[0])
+    check("last", got[1][2990:3010], want[1])
+
+
 def test_delta_numbers_that_are_none_stay_in_their_sequence_and_head():
     lengths = (50, 45)
     x, y = layer(95, 2, 2, 2, 16, 16)
