@@ -309,19 +309,20 @@ struct Job {
   long from, to;     // its blocks, counted in the sequence
   bool first, last;  // of the sequence's segments
 };
+__device__ __forceinline__ bool whole_sequences(const DeltaArgs& a) { return a.begin && a.first_segment[a.n_seq] == (int)a.n_seq; }
 // Segment `index` of all of them.
 __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& w) {
-  if (!a.segments) {
+  if (!a.segments || whole_sequences(a)) {   // no sequence is cut: nothing to search for
+    if (index >= a.n_seq) return false;
     if (a.begin && a.n_seq <= DELTA_ORDER) index = a.order[index];
     w.s = index, w.from = 0, w.to = first_block(a, index + 1) - first_block(a, index), w.first = w.last = true;
-    return index < a.n_seq;
+    return true;
   }
   size_t lo = 0, hi = a.n_seq;
   long size = a.segment;
   if (a.begin) {
     size = a.first_segment[a.n_seq + 1];
     if ((long)index >= a.first_segment[hi]) return false;
-    if (a.n_seq <= DELTA_ORDER && a.first_segment[hi] == (int)hi) index = a.order[index];   // no sequence is cut
     while (hi - lo > 1) {
       const size_t mid = (lo + hi) / 2;
       (a.first_segment[mid] <= (long)index ? lo : hi) = mid;
@@ -334,7 +335,6 @@ __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& 
   w.first = index == 0, w.last = (long)index + 1 == count;
   return true;
 }
-__device__ __forceinline__ bool whole_sequences(const DeltaArgs& a) { return a.begin && a.first_segment[a.n_seq] == (int)a.n_seq; }
 __device__ __forceinline__ size_t first_segment(const DeltaArgs& a, size_t s) { return a.begin ? a.first_segment[s] : 0; }
 
 constexpr int PLAN = 1024, NEAR = 4096;
