@@ -21,7 +21,7 @@
 // What bounds it: not HBM. A chunk of the chain takes 4 us on a compute unit (16,384 rows in 24 sequences, 16 heads of 128 x 128 bf16: 235 us
 // either way): vector instructions (a state's parts are formed anew for every chunk) keep the SIMDs busy for 45 % of that, the
 // matrix instructions for 30 %, and what is left is the two of them waiting for one another and for LDS, with two waves to a SIMD for want of
-// registers. The gradients (450 us of that case) wait for memory with one workgroup to a compute unit.
+// registers. The gradients (430 us of that case) wait for memory with one workgroup to a compute unit.
 #include "amp_ops.hip.h"
 
 namespace {
@@ -1031,7 +1031,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
 
 // From segment to segment: the state in front of the next (backward: the gradient behind the one before) is the map's share of this one's and what
 // the segment leaves of no state, which lies there already. 64 columns to a workgroup, whose waves share a map's parts in LDS; the next
-// map is on its way meanwhile: 7 us a step for 128 x 128.
+// map is on its way meanwhile: 8 us a step for 128 x 128.
 template <int KT, bool BACK>
 __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
   constexpr int PER = 32 * KT * KT * 8 / 256;
@@ -1090,9 +1090,9 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
 // the errors to follow is v.dv, so that G's gradient at a row is q.dq - v.dv, and at the last the state's own, <S', the state behind>, as well.
 // Of q.dq the part of dP is the sum over a row of dP o (Q K^T).
 //
-// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other, their sums kept in the workspace (each
-// thread its own). Values, their gradients and the states pass in steps of 32 columns, the next on its way meanwhile, its operands in the other
-// half of the LDS. What becomes dq and dk alone, which are rounded to the inputs' type, is formed from two parts where that is a type
+// Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other, their sums kept in LDS where there
+// is room and in the workspace where not (each thread its own; 107 of 500 us where all were in the workspace). Values, their gradients and
+// the states pass in steps of 32 columns, the next on its way meanwhile, its operands in the other half of the LDS. What becomes dq and dk alone, which are rounded to the inputs' type, is formed from two parts where that is a type
 // of 16 bits (2^-16 of the terms are left out); what becomes ddecay too, in 32 bits, from all.
 template <class T, int KT, int WIDTH>
 __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
@@ -1196,7 +1196,7 @@ __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
       for (int f = 0; f < KT; ++f) qk[k] = mma<3>(kq.along(16 * it, f), km.along(16 * jt, f), qk[k]);
     }
   int turn = 0;
-  // the group's sums: dq's and dk's 16 values of this thread, and dP's and dM's 12
+  // the group's sums: dq's and dk's 16 values of this thread each, and dP's and dM's 12
   float* kept = a.kept + ((w.index * a.key_heads + hk) * 44) * 512;
   v4f dq[4], dr[4], dc[4], pair[3];
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
