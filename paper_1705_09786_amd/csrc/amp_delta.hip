@@ -248,8 +248,10 @@ __device__ __forceinline__ void span(const DeltaArgs& a, size_t s, long& b, long
   b = x < 0 ? 0 : x > e ? e : x;
   e = y < b ? b : y > e ? e : y;
 }
-// Blocks in front of a sequence, at most the workspace's number of them.
-__device__ __forceinline__ long first_block(const DeltaArgs& a, size_t s) { return a.begin ? a.first[s] : s ? (long)a.blocks : 0; }
+__host__ __device__ inline long blocks_of(long rows) { return (rows + B - 1) / B; }
+// Blocks in front of a sequence, at most the workspace's number of them. (That number, a.blocks, is a bound: one sequence of a multiple of 64 rows
+// has one block less.)
+__device__ __forceinline__ long first_block(const DeltaArgs& a, size_t s) { return a.begin ? a.first[s] : s ? blocks_of((long)a.rows) : 0; }
 
 // `first`: the plan's or, without sequences' bounds, nothing.
 __device__ __forceinline__ bool search_block(const DeltaArgs& a, const int* first, size_t index, Block& w) {
@@ -303,6 +305,8 @@ __host__ __device__ inline long segment_blocks(long longest, long all, long work
   while (root * root * 4 < longest) ++root;
   return root > share ? root : share;
 }
+// Segments of a sequence, the whole of one that is not cut.
+__host__ __device__ inline long segments_of(long blocks, long size) { return blocks > size ? (blocks + size - 1) / size : 1; }
 
 struct Job {
   size_t s;          // its sequence
@@ -329,7 +333,7 @@ __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& 
     }
     index -= a.first_segment[lo];
   }
-  const long blocks = first_block(a, lo + 1) - first_block(a, lo), count = blocks > size ? (blocks + size - 1) / size : 1;
+  const long blocks = first_block(a, lo + 1) - first_block(a, lo), count = segments_of(blocks, size);
   if ((long)index >= count) return false;
   w.s = lo, w.from = (long)index * size, w.to = w.from + size < blocks ? w.from + size : blocks;
   w.first = index == 0, w.last = (long)index + 1 == count;
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
     const size_t s = s0 + threadIdx.x;
     long b = 0, e = 0;
     if (s < a.n_seq) span(a, s, b, e);
-    const long mine = (e - b + B - 1) / B, at = sum_in_front(mine, base, part);
+    const long mine = blocks_of(e - b), at = sum_in_front(mine, base, part);
     longest = mine > longest ? mine : longest;
     inside += e - b;
     if (s < a.n_seq) {
@@ -409,7 +413,7 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
     const size_t s = s0 + threadIdx.x;
     long blocks = 0;
     if (s < a.n_seq) blocks = near[s + 1] - near[s];   // written by this workgroup, a barrier ago
-    const long count = s < a.n_seq ? (blocks > size ? (blocks + size - 1) / size : 1) : 0, at = sum_in_front(count, base, part);
+    const long count = s < a.n_seq ? segments_of(blocks, size) : 0, at = sum_in_front(count, base, part);
     if (s < a.n_seq) a.first_segment[s] = (int)at;
   }
   if (threadIdx.x == 0) a.first_segment[a.n_seq] = (int)base, a.first_segment[a.n_seq + 1] = (int)size;
@@ -1040,7 +1044,7 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
   if (whole_sequences(a)) return;
   const size_t s = blockIdx.x / a.heads;
   const long size = a.begin ? a.first_segment[a.n_seq + 1] : a.segment, blocks = first_block(a, s + 1) - first_block(a, s);
-  const long count = blocks > size ? (blocks + size - 1) / size : 1;
+  const long count = segments_of(blocks, size);
   if (count < 3) return;
   const int col = (blockIdx.y * 4 + threadIdx.x / 64) * 16 + threadIdx.x % 16;
   const size_t base = first_segment(a, s);
@@ -1584,9 +1588,9 @@ hipError_t plan(DeltaArgs& a, hipStream_t stream) {
   if (a.begin) {
     e = launch(delta_plan_kernel, dim3(1), dim3(PLAN), 0, stream, a, work);
   } else if (a.segments) {
-    const long blocks = (long)((a.rows + B - 1) / B);
+    const long blocks = blocks_of((long)a.rows);
     a.segment = segment_blocks(blocks, blocks, work);
-    a.segments = a.n_seq && blocks > a.segment ? (size_t)((blocks + a.segment - 1) / a.segment) : 0;
+    a.segments = a.n_seq && blocks > a.segment ? (size_t)segments_of(blocks, a.segment) : 0;
   }
   const size_t groups = (a.rows + 3) / 4;
   if (e == hipSuccess && a.zero_others && a.rows && (a.begin || !a.n_seq))

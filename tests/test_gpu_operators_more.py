@@ -272,6 +272,24 @@ def test_delta_sequences_cut_into_segments(dtype, sequences):
     assert all(same_bits(p, q) for p, q in zip(got, both(x, y, where, 1)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,heads", [(1536, 1), (2048, 2), (4096, 1)])
+def test_delta_without_bounds_in_whole_segments(dtype, rows, heads):
+    """Rows that whole blocks and whole segments make up: one sequence is what its offsets say it is, to the last segment."""
+    x, y = layer(rows, 1, heads, 1, 24, 20, dtype, decay=0.001)
+    got = both(x, y, None, 1)
+    assert all(same_bits(p, q) for p, q in zip(got, both(x, y, offsets(rows), 1)))
+    against(x, y, None, 1, got)
+
+
+@pytest.mark.parametrize("rows,heads,dk,dv", [(2048, 16, 128, 128), (8192, 4, 64, 64), (16384, 2, 50, 75), (32768, 8, 16, 16)])
+def test_delta_without_bounds_is_one_sequence_of_all_rows(rows, heads, dk, dv):
+    x, y = layer(rows, 1, heads, heads, dk, dv, torch.bfloat16, decay=0.001)
+    x, y = ({k: v.cuda() for k, v in t.items()} for t in (x, y))
+    got, want = both(x, y, None, heads), both(x, y, offsets(rows), heads)
+    assert all(same_bits(p, q) for p, q in zip(got, want)) and all(g.isfinite().all() for g in got)
+
+
 # ------------------------------------------------------------------ policy loss
 def tokens(rows, classes, dtype=torch.float32, seed=0, temperature=1.0):
     logits = rand(rows, classes, seed=seed, scale=1.5)
