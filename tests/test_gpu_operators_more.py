@@ -412,6 +412,23 @@ def test_policy_far_ratios_and_open_limits():
     policy_against(x, y, 0.1, (1.0, INF))
 
 
+@pytest.mark.parametrize("classes", [40, 5000, 140003])
+def test_policy_class_without_probability(classes):
+    """Without `old` the ratio is 1 whatever the class's probability is: 0, a part of a bit, or all there is."""
+    x, y = tokens(4, classes)
+    x["logits"][0, int(x["index"][0])] = -INF
+    x["logits"][1, int(x["index"][1])] = -1e4
+    x["logits"][2] = -INF
+    x["logits"][2, int(x["index"][2])] = 0.0
+    x["old"], y["reference"] = None, None
+    got = policy_against(x, y)
+    assert got[1][0] == -INF and got[0][0] == -(x["advantage"] * y["weight"])[0]
+    x["logits"][3, 0] = NAN   # a log-probability that is no number leaves no loss and no gradient
+    x["index"][3] = 1
+    got = ops.policy_loss(x["logits"].cuda(), x["index"].cuda(), None, x["advantage"].cuda())
+    assert all(g[3].isnan().any() for g in got) and all(g[:3].isfinite().all() for g in (got[0], got[2]))
+
+
 # ------------------------------------------------------------------ clipping
 def some_tensors(sizes, dtype, seed=0, scale=1.0):
     return [rand(math.prod(s) if isinstance(s, tuple) else s, seed=seed + i, dtype=dtype, scale=scale).reshape(s) for i, s in enumerate(sizes)]
