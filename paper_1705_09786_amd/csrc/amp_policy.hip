@@ -46,7 +46,7 @@ __device__ __forceinline__ Row finish(const PolicyArgs& a, size_t r, float w, fl
   // without `old` the ratio is 1, whatever the probability: also where that is 0 (a log-probability that is no number goes on)
   const double adv = a.advantage[r], d = a.old ? lp - (double)a.old[r] : isnan(lp) ? lp : 0.0;
   // the ratio counts up to its limit on the side that the advantage asks for (a number that is none goes on)
-  const bool limited = adv >= 0.0 ? d > a.log_high : d < a.log_low;
+  const bool limited = adv >= 0.0 ? d > a.log_high : adv < 0.0 && d < a.log_low;
   const double ratio = limited ? (adv >= 0.0 ? a.high : a.low) : exp(d);
   double loss = -adv * ratio, by_lp = limited ? 0.0 : -adv * ratio;
   if (a.reference) {

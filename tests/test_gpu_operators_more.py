@@ -429,6 +429,16 @@ def test_policy_class_without_probability(classes):
     assert all(g[3].isnan().any() for g in got) and all(g[:3].isfinite().all() for g in (got[0], got[2]))
 
 
+def test_policy_advantage_that_is_no_number():
+    """On neither side of a limit: loss and gradient are no numbers, however far the ratio is."""
+    x, y = tokens(3, 50)
+    x["advantage"][:] = NAN
+    lp = torch.log_softmax(x["logits"].double(), 1).gather(1, x["index"][:, None])[:, 0]
+    x["old"] = (lp + torch.tensor([-2.0, 0.0, 2.0])).float()
+    loss, _, grad = ops.policy_loss(*(x[k].cuda() for k in ("logits", "index", "old", "advantage")))
+    assert loss.isnan().all() and grad.isnan().all()
+
+
 # ------------------------------------------------------------------ clipping
 def some_tensors(sizes, dtype, seed=0, scale=1.0):
     return [rand(math.prod(s) if isinstance(s, tuple) else s, seed=seed + i, dtype=dtype, scale=scale).reshape(s) for i, s in enumerate(sizes)]
