@@ -3,8 +3,8 @@
 // Bound by HBM: a workgroup has one row of logits in registers between its sums and the gradient, so that the row is read once; where
 // there is no gradient, rows of any length go by once under a running maximum.  8,192 x 32,000 bf16: 193 us with the gradient (5.4 TB/s), 93
 // without (5.6); 2,048 x 151,111 fp16, whose rows are not aligned to their 16-byte groups, 139 without (4.5).  A term of the softmax is exp2 of (x - max) times a scale of two
-// floats: the sum's error stays near 2^-24 of nothing but the terms' own roundings, and sums beyond a thread's, the logarithm and what
-// follows it are in 64 bits, since a ratio next to its limit decides whether the row has a gradient at all.
+// floats, off by some units of 2^-24. In 32 bits at most 128 terms are added up, a thread's of a row in registers (32 of a row that goes by); sums
+// of more, the logarithm and what follows it are in 64, since a ratio next to its limit decides whether the row has a gradient at all.
 #include "amp_ops.hip.h"
 
 namespace {
@@ -167,7 +167,8 @@ __global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
   const long own = class_at(a, r);
   if ((w == 0.f && !a.logprob) || own < 0) return left_out<TPB, T>(a, r, dx, true);
   const float mine = widen(x[own]);
-  float m = -INFINITY, s = 0.f;
+  float m = -INFINITY;
+  double s = 0.0;   // of any number of terms
   // DEEP groups to the running maximum and its sum; of terms that are all 0 so far (a maximum of -infinity) nothing is left to rescale
   const auto add = [&](const Vec<T>(&v)[DEEP], auto in) {
     float most = m;
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
 #pragma unroll
       for (int k = 0; k < N; ++k) most = fmaxf(most, in(j, k) ? get(v[j], k) : -INFINITY);
     const float origin = most == -INFINITY ? 0.f : most;
-    if (most > m) s *= m == -INFINITY ? 1.f : scale.term(m, most);
+    if (most > m) s *= m == -INFINITY ? 1.0 : (double)scale.term(m, most);
     m = most;
     float t[2] = {0.f, 0.f};
 #pragma unroll
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
         const float e = scale.term(get(v[j], k), origin);
         t[k & 1] += in(j, k) ? e : 0.f;
       }
-    s += t[0] + t[1];
+    s += (double)(t[0] + t[1]);
   };
   constexpr long TURN = (long)DEEP * TPB * N;
   long c0 = threadIdx.x * N;
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < NW; ++i) m = fmaxf(m, top[i]);
-  double sum = mt == -INFINITY ? (double)s : (double)s * scale.term(mt, m);
+  double sum = mt == -INFINITY ? s : s * scale.term(mt, m);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;

@@ -439,6 +439,26 @@ def test_policy_advantage_that_is_no_number():
     assert loss.isnan().all() and grad.isnan().all()
 
 
+def test_policy_very_long_row():
+    """2^24 classes, all but the first 0.3 below those: a thread's sum has thousands of equal terms, whose roundings in 32 bits would all point the
+    same way. Allowed: a term's own units (more_reference.policy), eight additions of them in 32 bits, and the result's rounding."""
+    classes, high, advantage, far = 1 << 24, 1 << 14, 2.0, 0.3
+    x = torch.full((1, classes), -far)
+    x[0, :high] = 0.0
+    index = torch.tensor([classes - 5])
+    far = -float(x[0, -1])   # as 32 bits have it
+    lp = -far - math.log((classes - high) * math.exp(-far) + high)
+    units = 4 + 3 * far + 8
+    want = torch.tensor([lp], dtype=torch.float64), torch.tensor([units], dtype=torch.float64)
+    on = x.cuda(), index.cuda()
+    check("logprob", ops.token_logprob(*on), want)
+    _, got, grad = ops.policy_loss(*on, None, torch.tensor([advantage], device="cuda"))
+    check("logprob", got, want)
+    value = advantage * torch.exp(x.double() + far + lp)
+    value[0, -5] = -advantage * (1 - math.exp(lp))
+    check("dlogits", grad, (value, (2 * units + 4) * value.abs()))
+
+
 # ------------------------------------------------------------------ clipping
 def some_tensors(sizes, dtype, seed=0, scale=1.0):
     return [rand(math.prod(s) if isinstance(s, tuple) else s, seed=seed + i, dtype=dtype, scale=scale).reshape(s) for i, s in enumerate(sizes)]
