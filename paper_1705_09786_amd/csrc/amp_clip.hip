@@ -6,6 +6,8 @@
 // second reading goes through the tensors from the last to the first, so that it begins with what the memory-side cache has last seen.
 // 97 tensors of 314 million floats together: the norm in 217 us (5.8 TB/s); 600 of 302 million bf16 with results: 110 us for the norm, 190 for
 // the results, and 390 with what the host does for 600 tensors.
+#include <float.h>
+
 #include "amp_ops.hip.h"
 
 namespace {
@@ -81,14 +83,15 @@ __global__ __launch_bounds__(JOIN) void clip_join_kernel(double* sums, unsigned 
   sums[n] = s > max_norm && s < INFINITY ? max_norm / s : 1.0;
 }
 
-template <class T>
-__device__ __forceinline__ void scaled(const T* p, T* o, size_t n, float f) {
+// F: float, or, for a factor that a normal float does not hold (its results may well be such), double.
+template <class F, class T>
+__device__ __forceinline__ void scaled(const T* p, T* o, size_t n, F f) {
   constexpr int N = Vec<T>::N, DEEP = 4;
   const auto times = [&](const Vec<T>& v) {
     float x[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = get(v, k) * f;
-    return f == 1.f ? v : pack<T>(x);
+    for (int k = 0; k < N; ++k) x[k] = (float)(get(v, k) * f);
+    return f == (F)1 ? v : pack<T>(x);
   };
   size_t i = threadIdx.x * N;
   for (; i + (DEEP - 1) * TPB * N + N <= n; i += DEEP * TPB * N) {
@@ -107,7 +110,11 @@ __global__ __launch_bounds__(TPB) void clip_scale_kernel(ClipList l, const doubl
   const float f = (float)*factor;
   if (!l.out[t] || (f == 1.f && l.out[t] == l.p[t])) return;
   const size_t begin = (size_t)(piece - l.first[t]) * l.piece, all = l.count[t] >> 2, n = all - begin < l.piece ? all - begin : l.piece;
-  OPS_BY_TYPE((int)(l.count[t] & 3), scaled((const T*)l.p[t] + begin, (T*)l.out[t] + begin, n, f));
+  if (f >= FLT_MIN || *factor == 0.0) {
+    OPS_BY_TYPE((int)(l.count[t] & 3), scaled((const T*)l.p[t] + begin, (T*)l.out[t] + begin, n, f));
+  } else {
+    OPS_BY_TYPE((int)(l.count[t] & 3), scaled((const T*)l.p[t] + begin, (T*)l.out[t] + begin, n, *factor));
+  }
 }
 
 // Elements of a piece: enough for a workgroup's time on them to hide its beginning, fewer where a call is a latency, more where the pieces would

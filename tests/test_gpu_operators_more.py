@@ -512,6 +512,22 @@ def test_clip_norms_that_floats_do_not_hold_on_the_way():
     assert ops.clip_gradients(zero, 1.0) == 0 and (zero[0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-6, 1e-8])
+def test_clip_by_factors_below_the_smallest_normal_float(dtype, max_norm):
+    """Norms of 1e38 and small limits: the factor is below 2^-126, the results are not."""
+    host = some_tensors((100, 7, 4099), dtype, scale=1.5e36)
+    grads = dev(*host)
+    norm = ops.clip_gradients(grads)
+    assert 5e37 < float(norm) < 2e38
+    out = [torch.empty_like(g) for g in grads]
+    ops.clip_gradients(grads, max_norm, out=out)
+    for o, w in zip(out, more.clip(host, max_norm)[1]):
+        check("out", o, w)
+    ops.clip_gradients(grads, max_norm)
+    assert all(same_bits(p, o) for p, o in zip(grads, out))
+
+
 # ------------------------------------------------------------------ together
 def problem(seed, dtype=torch.bfloat16):
     """A layer over packed sequences, with the classes that were drawn: every input of a training step."""
