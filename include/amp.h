@@ -665,9 +665,9 @@ int amp_policy_loss(int dtype, size_t rows, size_t classes, const void *logits, 
  * their squares, formed in 64 bits), and the tensors times
  * min(1, max_norm / norm): tensor i has n consecutive elements of dtype at p,
  * its result goes to out (NULL: none; p: in place).  A norm that is not finite
- * leaves the elements as they are, as one up to max_norm does.  norm: a float
- * (may be NULL).  Results overlap nothing but their own tensor.  The list is
- * read during the call. */
+ * as a float leaves the elements as they are, as one up to max_norm does.
+ * norm: a float (may be NULL).  Results overlap nothing but their own tensor.
+ * The list is read during the call. */
 typedef struct amp_tensor {
   const void *p;
   void *out;

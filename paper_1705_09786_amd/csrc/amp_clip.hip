@@ -80,7 +80,7 @@ __global__ __launch_bounds__(JOIN) void clip_join_kernel(double* sums, unsigned 
   for (int i = 0; i < JOIN / 64; ++i) s += part[i];
   s = sqrt(s);
   if (norm) *norm = (float)s;
-  sums[n] = s > max_norm && s < INFINITY ? max_norm / s : 1.0;
+  sums[n] = s > max_norm && (float)s < INFINITY ? max_norm / s : 1.0;   // finite as the caller sees it
 }
 
 // F: float, or, for a factor that a normal float does not hold (its results may well be such), double.

@@ -528,6 +528,17 @@ def test_clip_by_factors_below_the_smallest_normal_float(dtype, max_norm):
     assert all(same_bits(p, o) for p, o in zip(grads, out))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_clip_leaves_a_norm_beyond_floats(dtype):
+    """Finite numbers whose norm is not: as with any norm that is not finite, the elements stay."""
+    grads = [torch.full((10,), 3e38, dtype=dtype, device="cuda"), torch.ones(5, dtype=dtype, device="cuda")]
+    keep, out = [g.clone() for g in grads], [torch.zeros_like(g) for g in grads]
+    assert ops.clip_gradients(grads, 1.0, out=out) == INF
+    assert all(same_bits(p, q) for p, q in zip(out, keep))
+    assert ops.clip_gradients(grads, 1.0) == INF
+    assert all(same_bits(p, q) for p, q in zip(grads, keep))
+
+
 # ------------------------------------------------------------------ together
 def problem(seed, dtype=torch.bfloat16):
     """A layer over packed sequences, with the classes that were drawn: every input of a training step."""
