@@ -290,6 +290,41 @@ def test_delta_without_bounds_is_one_sequence_of_all_rows(rows, heads, dk, dv):
     assert all(same_bits(p, q) for p, q in zip(got, want)) and all(g.isfinite().all() for g in got)
 
 
+def some_lengths(n, most, seed):
+    return torch.randint(0, most + 1, (n,), generator=torch.Generator().manual_seed(seed)).tolist()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,heads,key_heads,dk,dv", [(70, 2, 2, 20, 70), (33, 4, 2, 50, 75), (12, 16, 16, 128, 66), (36, 4, 1, 100, 130)])
+def test_delta_more_than_128_chains(dtype, n, heads, key_heads, dk, dv):
+    """Sequences and heads enough for every type's workgroups of eight waves, at each size of a key."""
+    assert n * heads * ((dv + 127) // 128) > 128 and dv > 64
+    lengths = some_lengths(n, 70, n)
+    x, y = layer(sum(lengths), n, heads, key_heads, dk, dv, dtype)
+    against(x, y, offsets(*lengths), key_heads, both(x, y, offsets(*lengths), key_heads))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,key_heads,dk,dv", [((100, 33), 4, 1, 128, 40), ((70,), 3, 1, 50, 75), ((66, 5), 6, 2, 24, 20), ((65,), 5, 1, 3, 5),
+                                                           ((40,), 2, 1, 128, 3), ((90,), 1, 1, 8, 1024)])
+def test_delta_several_heads_to_a_key(dtype, lengths, heads, key_heads, dk, dv):
+    """A head between the first and the last both takes its key's sums and leaves them; rows narrower than four; the widest."""
+    x, y = layer(sum(lengths), len(lengths), heads, key_heads, dk, dv, dtype)
+    against(x, y, offsets(*lengths), key_heads, both(x, y, offsets(*lengths), key_heads))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,key_heads,dk,dv", [((1600,), 2, 1, 128, 130), ((1700, 100), 2, 2, 128, 128), ((1600, 300, 0, 40), 2, 2, 50, 75),
+                                                           ((1599,), 3, 1, 64, 64)])
+def test_delta_segments_of_wide_states(dtype, lengths, heads, key_heads, dk, dv):
+    """Maps and their join at every size of a key, for several heads and more columns than a workgroup has."""
+    x, y = layer(sum(lengths), len(lengths), heads, key_heads, dk, dv, dtype, decay=0.001)
+    where = None if len(lengths) == 1 else offsets(*lengths)
+    got = both(x, y, where, key_heads)
+    against(x, y, where, key_heads, got)
+    assert all(same_bits(p, q) for p, q in zip(got, both(x, y, where, key_heads)))
+
+
 # ------------------------------------------------------------------ policy loss
 def tokens(rows, classes, dtype=torch.float32, seed=0, temperature=1.0):
     logits = rand(rows, classes, seed=seed, scale=1.5)
