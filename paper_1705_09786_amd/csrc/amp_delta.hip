@@ -312,14 +312,16 @@ struct Job {
   size_t s;          // its sequence
   long from, to;     // its blocks, counted in the sequence
   bool first, last;  // of the sequence's segments
+  size_t slot;       // of a sequence that is cut: where its map and the state in front of it are
 };
+__device__ __forceinline__ size_t first_slot(const DeltaArgs& a, size_t s) { return a.begin ? a.first_slot[s] : 0; }
 __device__ __forceinline__ bool whole_sequences(const DeltaArgs& a) { return a.begin && a.first_segment[a.n_seq] == (int)a.n_seq; }
 // Segment `index` of all of them.
 __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& w) {
   if (!a.segments || whole_sequences(a)) {   // no sequence is cut: nothing to search for
     if (index >= a.n_seq) return false;
     if (a.begin && a.n_seq <= DELTA_ORDER) index = a.order[index];
-    w.s = index, w.from = 0, w.to = first_block(a, index + 1) - first_block(a, index), w.first = w.last = true;
+    w.s = index, w.from = 0, w.to = first_block(a, index + 1) - first_block(a, index), w.first = w.last = true, w.slot = 0;
     return true;
   }
   size_t lo = 0, hi = a.n_seq;
@@ -337,9 +339,9 @@ __device__ __forceinline__ bool find_job(const DeltaArgs& a, size_t index, Job& 
   if ((long)index >= count) return false;
   w.s = lo, w.from = (long)index * size, w.to = w.from + size < blocks ? w.from + size : blocks;
   w.first = index == 0, w.last = (long)index + 1 == count;
+  w.slot = count > 1 ? first_slot(a, lo) + index : 0;
   return true;
 }
-__device__ __forceinline__ size_t first_segment(const DeltaArgs& a, size_t s) { return a.begin ? a.first_segment[s] : 0; }
 
 constexpr int PLAN = 1024, NEAR = 4096;
 // Sums in front of every thread's value; `base` goes on by the sum of all.
@@ -407,16 +409,20 @@ __global__ __launch_bounds__(PLAN) void delta_plan_kernel(DeltaArgs a, long work
   __syncthreads();
   for (int w = 0; w < PLAN / 64; ++w) longest = max(longest, part[w]);
   __syncthreads();
-  const long size = segment_blocks(longest < all ? longest : all, all, work);
-  base = 0;
-  for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
-    const size_t s = s0 + threadIdx.x;
-    long blocks = 0;
-    if (s < a.n_seq) blocks = near[s + 1] - near[s];   // written by this workgroup, a barrier ago
-    const long count = s < a.n_seq ? segments_of(blocks, size) : 0, at = sum_in_front(count, base, part);
-    if (s < a.n_seq) a.first_segment[s] = (int)at;
+  // segments, and in the upper half those of sequences that are cut; of more of these than there are places, as only sequences out of order
+  // have, none is cut
+  for (long size = segment_blocks(longest < all ? longest : all, all, work);; size = (long)1 << 30) {
+    base = 0;
+    for (size_t s0 = 0; s0 < a.n_seq; s0 += PLAN) {
+      const size_t s = s0 + threadIdx.x;
+      long blocks = 0;
+      if (s < a.n_seq) blocks = near[s + 1] - near[s];   // written by this workgroup, a barrier ago
+      const long count = s < a.n_seq ? segments_of(blocks, size) : 0, at = sum_in_front(count > 1 ? count << 32 | count : count, base, part);
+      if (s < a.n_seq) a.first_segment[s] = (int)at, a.first_slot[s] = (int)(at >> 32);
+    }
+    if (threadIdx.x == 0) a.first_segment[a.n_seq] = (int)base, a.first_segment[a.n_seq + 1] = (int)size;
+    if (base >> 32 <= (long)a.slots) break;
   }
-  if (threadIdx.x == 0) a.first_segment[a.n_seq] = (int)base, a.first_segment[a.n_seq + 1] = (int)size;
 }
 
 // Rows of no sequence: a wave to a row, zeros in every output.
@@ -746,9 +752,9 @@ struct Columns {
   }
 };
 
-__device__ __forceinline__ float* front_of(const DeltaArgs& a, size_t segment, int h) { return a.fronts + state_at(a, segment, h); }
-__device__ __forceinline__ float* map_of(const DeltaArgs& a, size_t segment, int h) {
-  return a.maps + (segment * a.heads + h) * ((size_t)a.dk * a.dk);
+__device__ __forceinline__ float* front_of(const DeltaArgs& a, size_t slot, int h) { return a.fronts + state_at(a, slot, h); }
+__device__ __forceinline__ float* map_of(const DeltaArgs& a, size_t slot, int h) {
+  return a.maps + (slot * a.heads + h) * ((size_t)a.dk * a.dk);
 }
 
 // OUT: the chain with its outputs, from the states in front of the segments; else the segments' maps, and what they leave of no state.
@@ -772,7 +778,7 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
   if (e > b + (w.to - w.from) * B) e = b + (w.to - w.from) * B;
   State<KT> S;
   if (w.first) S.load(a.h0 ? a.h0 + state_at(a, w.s, h) : nullptr, a.dk, a.dv, col);
-  else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
+  else if (OUT) S.load(front_of(a, w.slot, h), a.dk, a.dv, col);
   else S.identity(m.map ? col : -1);
   const T* V = (const T*)a.v + (size_t)h * a.dv;
   const bool none = m.map || col >= a.dv;   // no values: a map's columns, and those behind the last
@@ -890,9 +896,9 @@ __global__ __launch_bounds__(64 * W, OUT ? 2 : 4) void delta_forward_kernel(Delt
   if (OUT) {
     if (a.last && w.last) S.store(a.last + state_at(a, w.s, h), a.dk, a.dv, col);
   } else if (m.map) {
-    S.store(map_of(a, segment, h), a.dk, a.dk, col);
+    S.store(map_of(a, w.slot, h), a.dk, a.dk, col);
   } else {
-    S.store(front_of(a, segment + 1, h), a.dk, a.dv, col);
+    S.store(front_of(a, w.slot + 1, h), a.dk, a.dv, col);
   }
 }
 
@@ -918,7 +924,7 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
   if (e > b + (w.to - w.from) * B) e = b + (w.to - w.from) * B;
   State<KT> S;   // the gradient of the state behind a chunk
   if (w.last) S.load(a.dlast ? a.dlast + state_at(a, w.s, h) : nullptr, a.dk, a.dv, col);
-  else if (OUT) S.load(front_of(a, segment, h), a.dk, a.dv, col);
+  else if (OUT) S.load(front_of(a, w.slot, h), a.dk, a.dv, col);
   else S.identity(m.map ? col : -1);
   const T* D = (const T*)a.dout + (size_t)h * a.dv;
   const bool none = m.map || col >= a.dv;
@@ -1027,9 +1033,9 @@ __global__ __launch_bounds__(64 * W) void delta_backward_kernel(DeltaArgs a) {
   if (OUT) {
     if (a.dh0 && w.first) S.store(a.dh0 + state_at(a, w.s, h), a.dk, a.dv, col);
   } else if (m.map) {
-    S.store(map_of(a, segment, h), a.dk, a.dk, col);
+    S.store(map_of(a, w.slot, h), a.dk, a.dk, col);
   } else {
-    S.store(front_of(a, segment - 1, h), a.dk, a.dv, col);
+    S.store(front_of(a, w.slot - 1, h), a.dk, a.dv, col);
   }
 }
 
@@ -1047,7 +1053,7 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
   const long count = segments_of(blocks, size);
   if (count < 3) return;
   const int col = (blockIdx.y * 4 + threadIdx.x / 64) * 16 + threadIdx.x % 16;
-  const size_t base = first_segment(a, s);
+  const size_t base = first_slot(a, s);
   const auto place = [&](long j) { return base + (BACK ? count - 1 - j : j); };
   Vec<float, 4> next[PER];
   const auto fetch = [&](long j) {
@@ -1529,12 +1535,14 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
 
 // ------------------------------------------------------------------ launches
 struct Sizes {
-  size_t blocks, segments, first, first_segment, order, table, matrices, scalars, sums, x, behind, kept, fronts, maps, bytes;   // offsets into the workspace
+  size_t blocks, segments, slots, first, first_segment, first_slot, order, table, matrices, scalars, sums, x, behind, kept, fronts, maps, bytes;   // offsets into the workspace
 };
 Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk, size_t dv, bool backward) {
   Sizes s;
   s.blocks = rows / B + (n < rows ? n : rows);
   s.segments = rows / B >= 24 ? s.blocks / DELTA_SEGMENT + n : 0;
+  // a sequence of b blocks is cut where b > 8, into at most (b + 7) / 8; it has more than 64 (b - 1) rows, 256 and more for each of those
+  s.slots = s.segments ? rows / (B * DELTA_SEGMENT / 2) : 0;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t p = at;
@@ -1543,6 +1551,7 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk,
   };
   s.first = take((n + 2) * sizeof(int));
   s.first_segment = take((n + 2) * sizeof(int));
+  s.first_slot = take(n * sizeof(int));
   s.order = take(n <= DELTA_ORDER ? n * sizeof(int) : 0);
   s.table = take(s.blocks * 2 * sizeof(int));
   s.matrices = take(s.blocks * heads * 4 * C * C * sizeof(float));
@@ -1552,8 +1561,8 @@ Sizes sizes_of(size_t rows, size_t n, size_t heads, size_t key_heads, size_t dk,
   s.x = take(backward ? s.blocks * heads * B * tiled * sizeof(float) : 0);
   s.behind = take(backward ? s.blocks * heads * dk * tiled * sizeof(float) : 0);
   s.kept = take(backward && heads > key_heads ? s.blocks * key_heads * 44 * 512 * sizeof(float) : 0);
-  s.fronts = take(s.segments * heads * dk * dv * sizeof(float));
-  s.maps = take(s.segments * heads * dk * dk * sizeof(float));
+  s.fronts = take(s.slots * heads * dk * dv * sizeof(float));
+  s.maps = take(s.slots * heads * dk * dk * sizeof(float));
   s.bytes = at;
   return s;
 }
@@ -1567,8 +1576,10 @@ void lay_out(DeltaArgs& a, bool backward) {
   a.fours = a.dk % 4 == 0 && a.dv % 4 == 0 ? FOURS : a.dk >= 4 && a.dv >= 4 ? ROWS : NARROW;
   a.blocks = s.blocks;
   a.segments = s.segments;
+  a.slots = s.slots;
   a.first = (int*)(w + s.first);
   a.first_segment = (int*)(w + s.first_segment);
+  a.first_slot = (int*)(w + s.first_slot);
   a.order = (int*)(w + s.order);
   a.table = (int*)(w + s.table);
   a.matrices = (float*)(w + s.matrices);

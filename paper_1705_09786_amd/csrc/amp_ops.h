@@ -90,8 +90,9 @@ struct DeltaArgs {
   // set by the launchers: whether dk and dv are multiples of 4, the workspace's parts, and where the carry's states begin
   int fours;
   size_t blocks, carry_states, segments;   // segments: at most, 0 = sequences stay whole
+  size_t slots;                            // places for the segments of sequences that are cut
   long segment;                            // blocks of one, where there is no plan
-  int *first, *first_segment, *order, *table;
+  int *first, *first_segment, *first_slot, *order, *table;
   float *matrices, *scalars, *x, *behind, *kept, *fronts, *maps;
   double* sums;
 };

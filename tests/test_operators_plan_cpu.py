@@ -113,6 +113,27 @@ extern "C" int divide(size_t rows, size_t n, size_t heads, size_t dk, size_t dv,
   }
   return 0;
 }
+
+// The places of a head's segments, and how many there are; -1: a job that is cut has none behind or in front of it.
+extern "C" long places(size_t rows, size_t n, size_t heads, const long* begin, const long* end, long* place, int* count) {
+  DeltaArgs a = {};
+  a.rows = rows, a.n_seq = n, a.heads = a.key_heads = (int)heads, a.dk = a.dv = 128;
+  a.begin = begin, a.end = end, a.index_bytes = 8;
+  const Sizes sizes = sizes_of(rows, n, heads, heads, 128, 128, false);
+  std::vector<char> ws(sizes.matrices);
+  memset(ws.data(), 0x3f, ws.size());
+  a.workspace = ws.data();
+  lay_out(a, false);
+  if (plan(a, nullptr) != hipSuccess) return -1;
+  const size_t launched = a.segments ? a.segments : a.n_seq;
+  *count = 0;
+  for (size_t i = 0; i < launched; ++i) {
+    Job w;
+    if (find_job(a, i, w) && !(w.first && w.last)) place[(*count)++] = (long)w.slot;
+  }
+  if (sizes.maps - sizes.fronts < sizes.slots * heads * 128 * 128 * 4 || sizes.bytes - sizes.maps < sizes.slots * heads * 128 * 128 * 4) return -1;
+  return (long)sizes.slots;
+}
 """
 
 
@@ -206,3 +227,44 @@ def test_sequences_by_their_bounds(library, heads):
         cut += check(library, rows + 50, begin, end, heads, 33, 40, 1)
     assert cut
     check(library, 10, [], [], heads)
+
+
+def places(lib, rows, begin, end, heads):
+    n = 1 if begin is None else len(begin)
+    place, count = np.zeros(rows // 64 + 2 * n, np.int64), np.zeros(1, np.int32)
+    at = lambda x: None if x is None else ct.c_void_p(x.ctypes.data)  # noqa: E731
+    if begin is not None:
+        begin, end = (np.ascontiguousarray(x, np.int64) for x in (begin, end))
+    size, lib.places.restype = ct.c_size_t, ct.c_long
+    there = lib.places(size(rows), size(n), size(heads), at(begin), at(end), at(place), at(count))
+    assert there >= 0
+    return there, place[:count[0]].tolist()
+
+
+def test_segments_of_sequences_that_are_cut_have_places(library):
+    """A place to each, one behind the other, within the workspace; sequences out of order, whose segments would be too many, are not cut."""
+    rng = np.random.default_rng(3)
+    cut = 0
+    for lengths in ([64 * 24], [1537], [2000, 0, 3, 2300], [513] * 2 + [1600], [40] * 100 + [2200, 577, 576] + [3] * 70,
+                    *(rng.integers(0, 4000, rng.integers(1, 12)).tolist() for _ in range(20))):
+        begin, end, rows = packed(lengths)
+        there, got = places(library, rows, begin, end, 1)
+        assert got == list(range(len(got))) and len(got) <= there
+        cut += bool(got)
+        there, got = places(library, rows, None, None, 1)
+        assert got == list(range(len(got))) and len(got) <= there
+    assert cut > 10
+    for rows in (1536, 4000, 70000):
+        for n in (2, 5, 300):
+            there, got = places(library, rows, [0] * n, [rows] * n, 1)
+            assert got == list(range(len(got))) and len(got) <= there
+
+
+def test_workspace_of_short_sequences():
+    """Nothing for segments but what sequences that are cut could take: of 1,000 times 20 rows, a place to 256 of the rows."""
+    from paper_1705_09786_amd import binding as B
+    shape, n = B.DeltaShape(B.BF16, 20000, 16, 16, 128, 128), ct.c_size_t()
+    assert B.lib().amp_gated_delta_workspace(shape, 1000, 0, ct.byref(n)) == B.AMP_OK
+    blocks, state = (20000 // 64 + 1000) * 16, 128 * 128 * 4
+    own = blocks * (4 * 32 * 32 * 4 + 4 * 64 * 4 + 64 * 8)   # N and P, powers, sums of decays
+    assert n.value <= own + 20000 // 256 * 16 * 2 * state + 100000
