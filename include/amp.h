@@ -603,6 +603,8 @@ int amp_distill_loss(int dtype, size_t rows, size_t classes, const void *logits,
  * 0 .. 2 and decays of at most 0 (-infinity forgets the state), where errors
  * do not grow; other values are taken as the formula has them.  A value that
  * is not finite may reach every row of its sequence and head, none of others.
+ * (In forward and backward passes numbers are sums of parts of 8 bits: parts
+ * below 2^-126 may count as 0, floats of 2^128 - 2^119 and more as infinite.)
  * dk 1 .. 128, dv 1 .. 1024, heads below 2^16, rows of fewer than 2^22
  * elements, strides of q, k, v, o and dout below 2^22 (but in a step), fewer
  * than 2^30 rows; at most 2^22 of (rows / 64 + sequences) x heads.

@@ -4,8 +4,9 @@
 // tensors that its arguments list, each piece's sum of squares has a place of its own in the workspace, in 64 bits (a square of a
 // float may be beyond floats, and a sum of 2^30 of them loses half its digits), and one workgroup adds the places up in their order.  The
 // second reading goes through the tensors from the last to the first, so that it begins with what the memory-side cache has last seen.
-// 97 tensors of 314 million floats together: the norm in 217 us (5.8 TB/s); 600 of 302 million bf16 with results: 110 us for the norm, 190 for
-// the results, and 390 with what the host does for 600 tensors.
+// 97 tensors of 314 million floats together: the norm in 217 us (5.8 TB/s). 600 of 302 million bf16: 400 us a call with results elsewhere, calls back
+// to back (147 for the norm and 226 for the results where a profiler lets each of the ten launches wait for the one in front); in place 236
+// where the norm is not beyond the limit, as long as the host takes for them.
 #include <float.h>
 
 #include "amp_ops.hip.h"

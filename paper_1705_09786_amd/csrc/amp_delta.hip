@@ -1103,7 +1103,8 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a) {
 // Eight waves, each with 16 columns of dq and dk; the heads that share a key one behind the other, their sums kept in LDS where there
 // is room and in the workspace where not (each thread its own; 107 of 500 us where all were in the workspace). Values, their gradients and
 // the states pass in steps of 32 columns, the next on its way meanwhile, its operands in the other half of the LDS. What becomes dq and dk alone, which are rounded to the inputs' type, is formed from two parts where that is a type
-// of 16 bits (2^-16 of the terms are left out); what becomes ddecay too, in 32 bits, from all.
+// of 16 bits (2^-16 of the terms are left out); what becomes ddecay too, in 32 bits, from all. All 256 registers of a lane are in use, and some
+// more in scratch: 2 .. 12 for types of 16 bits, 11 .. 51 for those of 32.
 template <class T, int KT, int WIDTH>
 __global__ __launch_bounds__(512) void delta_gradient_kernel(DeltaArgs a) {
   constexpr int P = In<T>::P, PK = sizeof(T) == 2 ? 2 : 3, LV = 32 + 8, Y = P, W = P + PK, PLANES = P + PK + 3;

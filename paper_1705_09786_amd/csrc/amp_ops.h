@@ -87,7 +87,8 @@ struct DeltaArgs {
   float *last, *dh0, *carry;
   void* workspace;
   DeltaZero zero[5];
-  // set by the launchers: whether dk and dv are multiples of 4, the workspace's parts, and where the carry's states begin
+  // set by the launchers: how rows are read four elements at a time (whether dk and dv are multiples of 4, at least 4, or less), the workspace's
+  // parts, and where the carry's states begin
   int fours;
   size_t blocks, carry_states, segments;   // segments: at most, 0 = sequences stay whole
   size_t slots;                            // places for the segments of sequences that are cut

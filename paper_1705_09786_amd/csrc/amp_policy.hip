@@ -1,8 +1,10 @@
 // The clipped policy loss with its gradient, and log-probabilities alone (include/amp.h has the formulas).
 //
-// Bound by HBM: a workgroup has one row of logits in registers between its sums and the gradient, so that the row is read once; where
-// there is no gradient, rows of any length go by once under a running maximum.  8,192 x 32,000 bf16: 193 us with the gradient (5.4 TB/s), 93
-// without (5.6); 2,048 x 151,111 fp16, whose rows are not aligned to their 16-byte groups, 139 without (4.5).  A term of the softmax is exp2 of (x - max) times a scale of two
+// Bound by HBM: a workgroup has one row of logits in registers between its sums and the gradient, so that the row is read once, up to 131,072
+// classes of 16 bits and 65,536 of 32 (longer ones are read again for their gradient); where there is no gradient, rows of any length go by
+// once under a running maximum.  8,192 x 32,000 bf16: 193 us with the gradient (5.4 TB/s), 100 without (5.2); rows that are not aligned to their
+// 16-byte groups, 2,048 x 151,111 fp16: 132 without (4.7), 363 with it (3.4 TB/s counted as one reading and one writing; f32 618, 4.0;
+// from registers 2,048 x 120,001 bf16 286, 3.4; 60,001 f32 222, 4.4).  A term of the softmax is exp2 of (x - max) times a scale of two
 // floats, off by some units of 2^-24. In 32 bits at most 128 terms are added up, a thread's of a row in registers (32 of a row that goes by); sums
 // of more, the logarithm and what follows it are in 64, since a ratio next to its limit decides whether the row has a gradient at all.
 #include "amp_ops.hip.h"
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(TPB) void policy_stream_kernel(PolicyArgs a) {
 
 // Which workgroup takes a row, by its 16-byte groups: with its gradient as few threads as hold it in registers, so that several rows are on a
 // compute unit; without, as few as read it in some turns of four groups (16,384 x 1,000 bf16: 296 us on 1,024 threads, 55 on 256, 19 on
-// 64; 8,192 x 32,000: 157, 93; 2,048 x 151,111 fp16: 159, 145 and 139 on 512).
+// 64; 8,192 x 32,000: 157, 93; 2,048 x 151,111 fp16: 159, 145 and 139 on 512, as they were compared, with a kernel that takes 132 now).
 template <class T>
 hipError_t run(const PolicyArgs& a, dim3 grid, hipStream_t stream) {
   const size_t groups = (a.classes + Vec<T>::N - 1) / Vec<T>::N;
